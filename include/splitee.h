@@ -309,6 +309,123 @@ int splitee_correction(float* C, int64_t ldc, const void* W, int w_type, int64_t
                        size_t workspace_bytes, void* stream);
 
 /*
+ * Projections with an epilogue, and the experts' projections of a mixture-of-experts layer.
+ *
+ * What follows the unmask of a projection, in the kernel that has it in registers.  With
+ * NW weight rows (N, or 2 N where gated),
+ *     Z = fl32(fl(A W^T) - C) + bias                        rows x NW, binary32
+ *     H = act(Z)                                            gated == 0 (NW = N)
+ *     H = act(Z[:, :N]) * Z[:, N:]                          gated != 0 (NW = 2 N: gate rows, then up rows)
+ *     Y = H + residual, rounded once to out_type (round to nearest even)
+ * every step in binary32; C, bias and residual may each be NULL (left out).  act, of one z:
+ *     NONE z;  SILU z / (1 + exp(-z));  GELU z (1 + erf(z / sqrt 2)) / 2;  RELU max(z, 0);
+ *     GELU_TANH z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2
+ * (a NaN stays a NaN, RELU's too; SILU and GELU of -inf are NaN, as the formulas say).
+ * Like the fused call's unmask, the epilogue computes on this GPU what the paper's deployment
+ * leaves to the trusted side.
+ */
+typedef enum {
+    SPLITEE_ACT_NONE = 0,
+    SPLITEE_ACT_SILU = 1,
+    SPLITEE_ACT_GELU = 2,
+    SPLITEE_ACT_GELU_TANH = 3,
+    SPLITEE_ACT_RELU = 4
+} splitee_act;
+
+typedef struct {
+    const float* C;        /* correction, rows x NW float32, or NULL; 16-byte aligned rows */
+    int64_t ldc;           /* >= NW, multiple of 4; unused without C */
+    const float* bias;     /* NW float32 (4-byte aligned), or NULL */
+    int64_t bias_stride;   /* splitee_grouped_linear: expert e's bias at bias + e * bias_stride, >= 0 */
+    const void* residual;  /* rows x N of out_type, or NULL; 16-byte aligned rows.  May be Y itself (same
+                              leading dimension): each element is read before it is written */
+    int64_t ldres;         /* >= N; unused without residual */
+    int32_t act;           /* splitee_act */
+    int32_t gated;         /* 0 or 1 */
+    int32_t out_type;      /* SPLITEE_F32 or SPLITEE_BF16: type of Y and residual */
+} splitee_epilogue_t;
+
+/* Workspace bytes needed by splitee_linear_epilogue (partial tiles of a split K), for either weight layout; 0
+ * when none is needed and on invalid arguments. */
+size_t splitee_epilogue_workspace_bytes(int64_t M, int64_t N, int64_t K, int prec, int gated);
+
+/*
+ * The product of splitee_masked_linear with the epilogue above: Y = epilogue(A W^T), M x N.
+ *   A, in_prec, lda     as splitee_mask writes them (planes M * lda apart); BF16 also serves plain
+ *                       bfloat16 activations, F32 plain binary32 ones
+ *   W, w_type, ldw      NW x K; bfloat16 (row-major or tiled), or float32 with F32 only; F32 takes
+ *                       row-major W (as splitee_masked_linear)
+ *   ep                  host, read during the call only; required
+ *   Y                   out, M x N of ep->out_type (ldy >= N), 16-byte aligned rows; must not overlap
+ *                       anything else that is read, but may be the residual
+ *   workspace           >= splitee_epilogue_workspace_bytes bytes, 256-byte aligned, no contents needed, none left
+ * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^22 (SPLITEE_ERR_UNSUPPORTED above).
+ * Results do not depend on timing: repeated calls give the same bits.
+ */
+int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void* W, int w_type, int64_t ldw,
+                            const splitee_epilogue_t* ep, void* Y, int64_t ldy, int64_t M, int64_t N, int64_t K,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The same product with an expert's own W for each group of rows: rows offsets[e] .. offsets[e + 1] - 1
+ * of Y, C and the residual belong to expert e, and row s takes row row_index[s] of A (row s itself where
+ * row_index is NULL):
+ *     Y[s] = epilogue(A[row_index[s]] W[e]^T),  offsets[e] <= s < offsets[e + 1]
+ *   A           a_rows x K as above (planes a_rows * lda apart); a_rows >= 1 where rows >= 1
+ *   row_index   device, rows int32 or NULL (then a_rows >= rows); an entry below 0 or past the end takes row 0 or
+ *               a_rows - 1 (no read leaves A)
+ *   offsets     device, experts + 1 int32 that do not decrease, offsets[0] >= 0; clamped to 0 .. rows.  As
+ *               splitee_route writes them.  Rows before offsets[0] and from offsets[experts] on are left as they were
+ *   experts     >= 0
+ *   W           expert e at element e * w_stride (a multiple of 8 for bfloat16, of 4 for float32), each as in
+ *               splitee_linear_epilogue; experts without rows are not read
+ *   rows        rows of Y, C, residual and row_index, >= 0
+ * No workspace: a tile's K reduction stays in one workgroup.  The row counts live on the device only: the
+ * call neither waits for them nor copies them.  Limits and results as in splitee_linear_epilogue.
+ */
+int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_rows, const int32_t* row_index,
+                           const int32_t* offsets, int64_t experts, const void* W, int w_type, int64_t ldw,
+                           int64_t w_stride, const splitee_epilogue_t* ep, void* Y, int64_t ldy, int64_t rows,
+                           int64_t N, int64_t K, void* stream);
+
+/*
+ * Router of a mixture-of-experts layer: the k experts of each token, their weights, and the order of rows
+ * that splitee_grouped_linear and splitee_combine take.
+ *   logits      T x E float32, leading dimension ldl >= E (4-byte aligned).  A logit of -inf or NaN masks its
+ *               expert: it is not chosen, and its score is 0
+ *   score       SOFTMAX: exp(l - max l) / sum over the row's experts; SIGMOID: 1 / (1 + exp(-l))
+ *   renorm      != 0: the chosen weights are divided by their sum (left 0 where that is 0)
+ *   experts     out, T x k int32: the k largest logits in falling order, equal ones by rising index;
+ *               -1 where fewer than k are not masked (a padding token: all of them)
+ *   weights     out, T x k float32; 0 beside -1
+ *   offsets     out, E + 1 int32: expert e's rows are offsets[e] .. offsets[e + 1] - 1, tokens in rising order
+ *   row_index   out, T * k int32: the token of each row; -1 from offsets[E] on
+ *   slot        out, T x k int32: the row of (token, choice); -1 beside -1
+ * experts, weights and slot are dense (leading dimension k).  1 <= k <= min(E, 64), E <= 1024
+ * (SPLITEE_ERR_UNSUPPORTED above), T k < 2^31.  T == 0 writes zero offsets.  workspace: >=
+ * splitee_route_workspace_bytes bytes, 256-byte aligned, no contents needed.
+ */
+typedef enum { SPLITEE_SCORE_SOFTMAX = 0, SPLITEE_SCORE_SIGMOID = 1 } splitee_score;
+size_t splitee_route_workspace_bytes(int64_t T, int64_t E, int64_t k);
+int splitee_route(const float* logits, int64_t ldl, int64_t T, int64_t E, int64_t k, int score, int renorm,
+                  int32_t* experts, float* weights, int32_t* offsets, int32_t* row_index, int32_t* slot,
+                  void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Weighted sum of a token's expert rows: Y[t] = residual[t] + sum over j of weights[t, j] H[slot[t, j]],
+ * in binary32, from 0 in rising j by fma, the residual last, rounded once to out_type.
+ *   H           h_rows x N, h_type SPLITEE_F32 or SPLITEE_BF16, leading dimension ldh; 16-byte aligned rows
+ *   slot        device, T x k int32 (dense); an entry below 0 or >= h_rows adds nothing
+ *   weights     device, T x k float32 (dense)
+ *   residual    T x N of out_type (ldres) or NULL; may be Y itself (same leading dimension)
+ *   Y           out, T x N of out_type, leading dimension ldy; must not overlap H
+ * 1 <= k <= 64, N below 2^22 (SPLITEE_ERR_UNSUPPORTED above).
+ */
+int splitee_combine(const void* H, int h_type, int64_t ldh, int64_t h_rows, const int32_t* slot, const float* weights,
+                    const void* residual, int64_t ldres, void* Y, int out_type, int64_t ldy, int64_t T, int64_t k,
+                    int64_t N, void* stream);
+
+/*
  * Binary64 variant of the fused call and the correction (SPLITEE_PREC_F64): for a
  * projection whose noise scale is too large for binary32 cancellation, as for the Down
  * projection under Theorem 3 (Sec. "The Case Against the Down Linear Projection": with

@@ -8,6 +8,7 @@ still works but every call raises.
 """
 import ctypes
 import os
+import typing
 
 import torch
 
@@ -33,6 +34,8 @@ EXPORTED = [
     "splitee_bank_info", "splitee_bank_load", "splitee_bank_close",
     "splitee_f64_workspace_bytes", "splitee_masked_linear_fused_f64", "splitee_correction_f64",
     "splitee_tiled_weights_bytes", "splitee_tile_weights", "splitee_masked_linear_fused_noalloc",
+    "splitee_epilogue_workspace_bytes", "splitee_linear_epilogue", "splitee_grouped_linear",
+    "splitee_route_workspace_bytes", "splitee_route", "splitee_combine",
 ]
 # test hooks (include/splitee_probe.h)
 EXPORTED_PROBE = ["splitee_transform_probe", "splitee_mfma_probe", "splitee_spectral_norm_probe"]
@@ -41,6 +44,11 @@ SPLITEE_PREC_F64 = 3
 SPLITEE_ERR_IO, SPLITEE_ERR_EXHAUSTED, SPLITEE_ERR_FORMAT, SPLITEE_ERR_BUSY = -8, -9, -10, -11
 SPLITEE_ERR_SCRATCH = -12
 SPLITEE_NOALLOC_SCRATCH_BYTES = 64 << 20
+SPLITEE_ACT_NONE, SPLITEE_ACT_SILU, SPLITEE_ACT_GELU, SPLITEE_ACT_GELU_TANH, SPLITEE_ACT_RELU = 0, 1, 2, 3, 4
+ACTS = {"none": SPLITEE_ACT_NONE, "silu": SPLITEE_ACT_SILU, "gelu": SPLITEE_ACT_GELU,
+        "gelu_tanh": SPLITEE_ACT_GELU_TANH, "relu": SPLITEE_ACT_RELU}
+SPLITEE_SCORE_SOFTMAX, SPLITEE_SCORE_SIGMOID = 0, 1
+SCORES = {"softmax": SPLITEE_SCORE_SOFTMAX, "sigmoid": SPLITEE_SCORE_SIGMOID}
 
 
 class BankInfo(ctypes.Structure):
@@ -53,6 +61,13 @@ class BankInfo(ctypes.Structure):
 
     def as_dict(self):
         return {name: getattr(self, name) for name, _ in self._fields_}
+
+
+class Epilogue(ctypes.Structure):
+    """splitee_epilogue_t"""
+    _fields_ = [("C", ctypes.c_void_p), ("ldc", ctypes.c_int64), ("bias", ctypes.c_void_p),
+                ("bias_stride", ctypes.c_int64), ("residual", ctypes.c_void_p), ("ldres", ctypes.c_int64),
+                ("act", ctypes.c_int32), ("gated", ctypes.c_int32), ("out_type", ctypes.c_int32)]
 
 
 class SpliteeError(RuntimeError):
@@ -115,6 +130,12 @@ def load():
         "splitee_spectral_norm_probe": (I, [P, I, I64, I64, I64, I, U64, U64, P, P, P, SZ, I64, P, P]),
         "splitee_masked_linear_fused_noalloc": (I, [P, I64, P, I, I64, P, I64, P, I64, I64, I64, I64, I, D, D,
                                                     U64, U64, U64, P, I, P]),
+        "splitee_epilogue_workspace_bytes": (SZ, [I64, I64, I64, I, I]),
+        "splitee_linear_epilogue": (I, [P, I, I64, P, I, I64, P, P, I64, I64, I64, I64, P, SZ, P]),
+        "splitee_grouped_linear": (I, [P, I, I64, I64, P, P, I64, P, I, I64, I64, P, P, I64, I64, I64, I64, P]),
+        "splitee_route_workspace_bytes": (SZ, [I64, I64, I64]),
+        "splitee_route": (I, [P, I64, I64, I64, I64, I, I, P, P, P, P, P, P, SZ, P]),
+        "splitee_combine": (I, [P, I, I64, I64, P, P, P, I64, P, I, I64, I64, I64, I64, P]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -158,7 +179,8 @@ def _check(fn, status):
 
 class TiledWeights:
     """A bfloat16 N x K weight matrix stored in the tiled order of
-    splitee_tile_weights (`data`, a flat device tensor).  Passed wherever a W tensor
+    splitee_tile_weights (`data`, a flat device tensor; for the experts of grouped_linear
+    one row of an experts x elements tensor each).  Passed wherever a W tensor
     is taken; shape, dtype, stride and data_ptr describe the logical matrix."""
 
     dtype = torch.bfloat16
@@ -418,6 +440,43 @@ def splitee_bank_close(bank):
     _check("splitee_bank_close", load().splitee_bank_close(bank))
 
 
+def splitee_epilogue_workspace_bytes(M, N, K, prec, gated):
+    return load().splitee_epilogue_workspace_bytes(M, N, K, prec, 1 if gated else 0)
+
+
+def splitee_linear_epilogue(A, in_prec, lda, W, w_type, ldw, ep, Y, ldy, M, N, K, workspace, workspace_bytes,
+                            stream=None):
+    """ep: an Epilogue."""
+    _check("splitee_linear_epilogue", load().splitee_linear_epilogue(
+        _ptr(A), in_prec, lda, _ptr(W), w_type, ldw, ctypes.byref(ep), _ptr(Y), ldy, M, N, K, _ptr(workspace),
+        workspace_bytes, _stream(stream)))
+
+
+def splitee_grouped_linear(A, in_prec, lda, a_rows, row_index, offsets, experts, W, w_type, ldw, w_stride, ep, Y, ldy,
+                           rows, N, K, stream=None):
+    """ep: an Epilogue."""
+    _check("splitee_grouped_linear", load().splitee_grouped_linear(
+        _ptr(A), in_prec, lda, a_rows, _ptr(row_index), _ptr(offsets), experts, _ptr(W), w_type, ldw, w_stride,
+        ctypes.byref(ep), _ptr(Y), ldy, rows, N, K, _stream(stream)))
+
+
+def splitee_route_workspace_bytes(T, E, k):
+    return load().splitee_route_workspace_bytes(T, E, k)
+
+
+def splitee_route(logits, ldl, T, E, k, score, renorm, experts, weights, offsets, row_index, slot, workspace,
+                  workspace_bytes, stream=None):
+    _check("splitee_route", load().splitee_route(
+        _ptr(logits), ldl, T, E, k, score, 1 if renorm else 0, _ptr(experts), _ptr(weights), _ptr(offsets),
+        _ptr(row_index), _ptr(slot), _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def splitee_combine(H, h_type, ldh, h_rows, slot, weights, residual, ldres, Y, out_type, ldy, T, k, N, stream=None):
+    _check("splitee_combine", load().splitee_combine(
+        _ptr(H), h_type, ldh, h_rows, _ptr(slot), _ptr(weights), _ptr(residual), ldres, _ptr(Y), out_type, ldy, T, k,
+        N, _stream(stream)))
+
+
 # ------------------------------------------------- tensor-level conveniences
 
 def _aligned_bytes(nbytes, device):
@@ -573,4 +632,181 @@ def masked_linear_fused(X, W, C, mech, sensitivity, epsilon, seed, stream_id, ro
     splitee_masked_linear_fused(X, X.stride(0), W, _wtype(W), W.stride(0), C, C.stride(0), Y,
                                 Y.stride(0), M, N, K, mech, sensitivity, epsilon, seed, stream_id,
                                 row0, eta_override, prec, ws[0], ws[1])
+    return Y
+
+
+# ---------------------------------------- projections with an epilogue, and experts
+
+_OUT = {torch.float32: SPLITEE_F32, torch.bfloat16: SPLITEE_BF16}
+
+
+def _expect(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _here(**tensors):
+    """Every tensor on the current device, whose stream the call takes."""
+    dev = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.device.index != dev:
+            raise ValueError("%s is on %s, not on the current device" % (name, t.device))
+
+
+def _matrix(name, t, shape, dtype):
+    _expect(tuple(t.shape) == shape and t.dtype == dtype, "%s: expected %s of %s" % (name, dtype, shape))
+    _expect(t.stride(-1) == 1 or shape[-1] <= 1, "%s: columns are not contiguous" % name)
+    per = 16 // t.element_size()
+    return t.stride(0) if shape[0] > 1 else -(-shape[1] // per) * per  # of a single row no pitch is used
+
+
+def _rows_out(rows, N, dtype, device):
+    """rows x N whose rows begin at multiples of 16 bytes."""
+    per = 16 // dtype.itemsize
+    ld = -(-N // per) * per
+    return torch.empty((rows, ld), dtype=dtype, device=device)[:, :N]
+
+
+def _operand(A, prec):
+    """(rows, K, leading dimension) of planes x rows x K as mask() returns them, or rows x K."""
+    planes = 3 if prec == SPLITEE_PREC_BF16X3 else 1
+    size = 4 if prec == SPLITEE_PREC_F32 else 2
+    _expect(prec in (SPLITEE_PREC_F32, SPLITEE_PREC_BF16, SPLITEE_PREC_BF16X3), "A: precision F32, BF16 or BF16X3")
+    _expect(A.dtype in ((torch.float32,) if size == 4 else (torch.bfloat16, torch.int16)), "A: dtype does not fit its precision")
+    _expect(A.dim() == 3 and A.shape[0] == planes or A.dim() == 2 and planes == 1, "A: expected planes x rows x K")
+    rows, K = A.shape[-2:]
+    lda = K if not rows or not K else A.stride(-2) if rows > 1 else A.stride(0) if planes > 1 else K
+    _expect(A.stride(-1) == 1 or K <= 1, "A: columns are not contiguous")
+    _expect(planes == 1 or not A.numel() or A.stride(0) == rows * lda, "A: planes are not one after another")
+    return rows, K, lda
+
+
+def _epilogue(rows, N, NW, C, bias, act, gated, residual, out_dtype, bias_stride=0):
+    _expect(out_dtype in _OUT, "out_dtype: float32 or bfloat16")
+    ep = Epilogue(act=ACTS[act] if isinstance(act, str) else act, gated=1 if gated else 0, out_type=_OUT[out_dtype])
+    if C is not None:
+        ep.ldc = _matrix("C", C, (rows, NW), torch.float32)
+        ep.C = _ptr(C)
+    if bias is not None:
+        ep.bias, ep.bias_stride = _ptr(bias), bias_stride
+    if residual is not None:
+        ep.ldres = _matrix("residual", residual, (rows, N), out_dtype)
+        ep.residual = _ptr(residual)
+    return ep
+
+
+def _out_width(NW, gated):
+    _expect(not gated or NW % 2 == 0, "W: a gated projection has as many gate as up rows")
+    return NW // 2 if gated else NW
+
+
+def linear_epilogue(A, prec, W, C=None, bias=None, act="none", gated=False, residual=None,
+                    out_dtype=torch.float32, ws=None, Y=None):
+    """epilogue(A W^T) (see splitee_linear_epilogue).  A: planes x M x K as mask() and noise_mask() return it, or
+    M x K bfloat16 or float32; W: N (gated: 2 N) x K, a tensor or TiledWeights; act a name of ACTS."""
+    M, K, lda = _operand(A, prec)
+    NW = W.shape[0]
+    _expect(len(W.shape) == 2 and W.shape[1] == K, "W: expected N x %d" % K)
+    _expect(W.stride(1) == 1 or K <= 1, "W: columns are not contiguous")
+    N = _out_width(NW, gated)
+    _here(A=A, W=W, C=C, bias=bias, residual=residual, Y=Y)
+    if bias is not None:
+        _expect(tuple(bias.shape) == (NW,) and bias.dtype == torch.float32 and (NW < 2 or bias.stride(0) == 1),
+                "bias: expected %d contiguous float32" % NW)
+    ep = _epilogue(M, N, NW, C, bias, act, gated, residual, out_dtype)
+    if Y is None:
+        Y = _rows_out(M, N, out_dtype, A.device)
+    ldy = _matrix("Y", Y, (M, N), out_dtype)
+    if ws is None:
+        nbytes = splitee_epilogue_workspace_bytes(M, N, K, prec, gated)
+        ws = (_aligned_bytes(nbytes, A.device) if nbytes else None, nbytes)
+    splitee_linear_epilogue(A, prec, lda, W, _wtype(W), W.stride(0) if NW > 1 and K else K, ep, Y, ldy, M, N, K, ws[0], ws[1])
+    return Y
+
+
+def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="none", gated=False, residual=None,
+                   out_dtype=torch.float32, Y=None):
+    """Each expert's rows times its own W, with the epilogue (see splitee_grouped_linear).  W: experts x N (gated:
+    2 N) x K, or the TiledWeights of tile_experts; offsets and row_index as route() returns them (without
+    row_index, A is already in their order); bias experts x N (2 N)."""
+    a_rows, K, lda = _operand(A, prec)
+    tiled = isinstance(W, TiledWeights)
+    _expect(len(W.shape) == (2 if tiled else 3) and W.shape[-1] == K, "W: expected experts x N x %d" % K)
+    experts = (W.data if tiled else W).shape[0]
+    NW = W.shape[-2]
+    N = _out_width(NW, gated)
+    _here(A=A, W=W, offsets=offsets, row_index=row_index, C=C, bias=bias, residual=residual, Y=Y)
+    for name, t, n in (("offsets", offsets, experts + 1), ("row_index", row_index, None)):
+        _expect(t is None or t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and n in (None, t.numel()),
+                "%s: expected contiguous int32%s" % (name, " of experts + 1" if n else ""))
+    rows = a_rows if row_index is None else row_index.numel()
+    if tiled:
+        _expect(W.data.dim() == 2 and W.data.shape[1] * 2 >= splitee_tiled_weights_bytes(NW, K) and W.data.stride(1) == 1,
+                "W: expected experts x elements of tiled weights")
+        ldw, w_stride = K, W.data.stride(0)
+    else:
+        _expect(W.stride(2) == 1 or K <= 1, "W: columns are not contiguous")
+        ldw, w_stride = W.stride(1) if NW > 1 and K else K, W.stride(0) if experts > 1 and K else 0
+    if bias is not None:
+        _expect(tuple(bias.shape) == (experts, NW) and bias.dtype == torch.float32 and (NW < 2 or bias.stride(1) == 1),
+                "bias: expected float32 of experts x %d" % NW)
+    ep = _epilogue(rows, N, NW, C, bias, act, gated, residual, out_dtype, 0 if bias is None else bias.stride(0))
+    if Y is None:
+        Y = _rows_out(rows, N, out_dtype, A.device)
+    ldy = _matrix("Y", Y, (rows, N), out_dtype)
+    splitee_grouped_linear(A, prec, lda, a_rows, row_index, offsets, experts, W, _wtype(W), ldw, w_stride, ep, Y, ldy,
+                           rows, N, K)
+    return Y
+
+
+def tile_experts(W):
+    """experts x N x K bfloat16 in the tiled order, an expert a row of the TiledWeights' data."""
+    E, N, K = W.shape
+    data = torch.empty((E, splitee_tiled_weights_bytes(N, K) // 2), dtype=torch.bfloat16, device=W.device)
+    for e in range(E):
+        splitee_tile_weights(W[e], W.stride(1), N, K, data[e])
+    return TiledWeights(data, N, K)
+
+
+class Routes(typing.NamedTuple):
+    """What splitee_route writes."""
+    experts: torch.Tensor    # T x k int32
+    weights: torch.Tensor    # T x k float32
+    offsets: torch.Tensor    # experts + 1 int32
+    row_index: torch.Tensor  # T * k int32
+    slot: torch.Tensor       # T x k int32
+
+
+def route(logits, k, score="softmax", renorm=True, ws=None):
+    """The k experts of every token and the order of the rows (see splitee_route).  logits: T x experts float32."""
+    _expect(logits.dim() == 2 and logits.dtype == torch.float32, "logits: expected float32 of tokens x experts")
+    T, E = logits.shape
+    _expect(logits.stride(1) == 1 or E <= 1, "logits: columns are not contiguous")
+    _here(logits=logits)
+    dev, i32 = logits.device, torch.int32
+    r = Routes(torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=torch.float32, device=dev),
+               torch.empty(E + 1, dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev),
+               torch.empty((T, k), dtype=i32, device=dev))
+    if ws is None:
+        nbytes = splitee_route_workspace_bytes(T, E, k)
+        ws = (_aligned_bytes(nbytes, dev), nbytes)
+    splitee_route(logits, logits.stride(0) if T > 1 else E, T, E, k, SCORES[score] if isinstance(score, str) else score,
+                  renorm, r.experts, r.weights, r.offsets, r.row_index, r.slot, ws[0], ws[1])
+    return r
+
+
+def combine(H, slot, weights, residual=None, out_dtype=torch.float32, Y=None):
+    """Y[t] = residual[t] + sum_j weights[t, j] H[slot[t, j]] (see splitee_combine)."""
+    _expect(H.dim() == 2 and H.dtype in _OUT and out_dtype in _OUT, "H, out_dtype: float32 or bfloat16")
+    _expect(slot.dim() == 2 and slot.dtype == torch.int32 and slot.is_contiguous() and weights.shape == slot.shape
+            and weights.dtype == torch.float32 and weights.is_contiguous(),
+            "slot, weights: expected contiguous int32 and float32 of tokens x k")
+    (h_rows, N), (T, k) = H.shape, slot.shape
+    _here(H=H, slot=slot, weights=weights, residual=residual, Y=Y)
+    ldh = _matrix("H", H, (h_rows, N), H.dtype)
+    ldres = _matrix("residual", residual, (T, N), out_dtype) if residual is not None else 0
+    if Y is None:
+        Y = _rows_out(T, N, out_dtype, H.device)
+    splitee_combine(H, _OUT[H.dtype], ldh, h_rows, slot, weights, residual, ldres, Y, _OUT[out_dtype],
+                    _matrix("Y", Y, (T, N), out_dtype), T, k, N)
     return Y

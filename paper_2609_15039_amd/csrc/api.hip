@@ -4,6 +4,7 @@
 
 #include <mutex>
 
+#include "api_checks.hpp"
 #include "common.hpp"
 #include "splitee_probe.h"
 
@@ -13,14 +14,9 @@ size_t skinny_counter_bytes(int64_t M, int64_t N, int64_t K, int prec, int w_typ
 
 namespace {
 
-constexpr int64_t MAX_DIM = int64_t(1) << 30;
 constexpr int MAX_POWER_ITERS = 1 << 20;
 
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 inline size_t align256(size_t b) { return (b + 255) / 256 * 256; }
-inline bool pitch16(int64_t ld, int64_t elsize) { return (ld * elsize) % 16 == 0; }
-inline hipStream_t as_stream(void* s) { return reinterpret_cast<hipStream_t>(s); }
-
 inline bool valid_mech(int mech)
 {
     return mech == SPLITEE_MECH_LAPLACE || mech == SPLITEE_MECH_GAUSSIAN || mech == SPLITEE_MECH_NONE;
@@ -33,19 +29,6 @@ inline int check_noise_args(int mech, double sensitivity, double epsilon)
     if (!(sensitivity >= 0.0) || !isfinite(sensitivity)) return SPLITEE_ERR_ARG;
     return SPLITEE_OK;
 }
-
-inline bool dims_ok(int64_t M, int64_t N, int64_t K)
-{
-    return M >= 0 && N >= 0 && K >= 0 && M <= MAX_DIM && N <= MAX_DIM && K <= MAX_DIM;
-}
-
-inline int64_t prec_elsize(int prec) { return prec == SPLITEE_PREC_F64 ? 8 : prec == SPLITEE_PREC_F32 ? 4 : 2; }
-inline int64_t prec_planes(int prec) { return prec == SPLITEE_PREC_BF16X3 ? 3 : 1; }
-inline bool valid_prec(int prec)
-{
-    return prec == SPLITEE_PREC_F32 || prec == SPLITEE_PREC_BF16 || prec == SPLITEE_PREC_BF16X3;
-}
-inline bool valid_dtype(int t) { return t == SPLITEE_F32 || t == SPLITEE_BF16 || t == SPLITEE_BF16_TILED; }
 
 // Skinny kernel for decode-sized M with bfloat16 operands, tiled kernel otherwise.
 inline bool use_skinny(int64_t M, int prec) { return M <= 16 && prec != SPLITEE_PREC_F32; }
@@ -78,21 +61,6 @@ size_t gemm_ws_any(int64_t M, int64_t N, int64_t K, int prec)
 size_t gemm_counters(int64_t M, int64_t N, int64_t K, int prec, int w_type)
 {
     return use_skinny(M, prec) ? splitee_host::skinny_counter_bytes(M, N, K, prec, w_type) : 0;
-}
-
-// GEMM operand checks shared by the GEMM entry points.
-int check_w(const void* W, int w_type, int64_t ldw, int64_t K, int prec)
-{
-    if (!valid_dtype(w_type)) return SPLITEE_ERR_DTYPE;
-    if (w_type == SPLITEE_BF16_TILED) { // ldw is not used: the layout is fixed by N and K
-        if (prec == SPLITEE_PREC_F32) return SPLITEE_ERR_UNSUPPORTED;
-        return aligned16(W) ? SPLITEE_OK : SPLITEE_ERR_ALIGN;
-    }
-    if (prec != SPLITEE_PREC_F32 && w_type != SPLITEE_BF16) return SPLITEE_ERR_UNSUPPORTED;
-    const int64_t wes = w_type == SPLITEE_F32 ? 4 : 2;
-    if (ldw < K) return SPLITEE_ERR_SHAPE;
-    if (!aligned16(W) || !pitch16(ldw, wes)) return SPLITEE_ERR_ALIGN;
-    return SPLITEE_OK;
 }
 
 // GEMM (+ unmask) on a masked input already in memory.
