@@ -359,7 +359,7 @@ size_t splitee_epilogue_workspace_bytes(int64_t M, int64_t N, int64_t K, int pre
  *   Y                   out, M x N of ep->out_type (ldy >= N), 16-byte aligned rows; must not overlap
  *                       anything else that is read, but may be the residual
  *   workspace           >= splitee_epilogue_workspace_bytes bytes, 256-byte aligned, no contents needed, none left
- * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^22 (SPLITEE_ERR_UNSUPPORTED above).
+ * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^20 (SPLITEE_ERR_UNSUPPORTED above).
  * Results do not depend on timing: repeated calls give the same bits.
  */
 int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void* W, int w_type, int64_t ldw,
@@ -373,7 +373,8 @@ int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void*
  *     Y[s] = epilogue(A[row_index[s]] W[e]^T),  offsets[e] <= s < offsets[e + 1]
  *   A           a_rows x K as above (planes a_rows * lda apart); a_rows >= 1 where rows >= 1
  *   row_index   device, rows int32 or NULL (then a_rows >= rows); an entry below 0 or past the end takes row 0 or
- *               a_rows - 1 (no read leaves A)
+ *               a_rows - 1 (no read leaves A).  With it a plane of A (a_rows * lda elements) must be below 2 GB
+ *               (SPLITEE_ERR_UNSUPPORTED above)
  *   offsets     device, experts + 1 int32 that do not decrease, offsets[0] >= 0; clamped to 0 .. rows.  As
  *               splitee_route writes them.  Rows before offsets[0] and from offsets[experts] on are left as they were
  *   experts     >= 0
@@ -419,7 +420,7 @@ int splitee_route(const float* logits, int64_t ldl, int64_t T, int64_t E, int64_
  *   weights     device, T x k float32 (dense)
  *   residual    T x N of out_type (ldres) or NULL; may be Y itself (same leading dimension)
  *   Y           out, T x N of out_type, leading dimension ldy; must not overlap H
- * 1 <= k <= 64, N below 2^22 (SPLITEE_ERR_UNSUPPORTED above).
+ * 1 <= k <= 64, N below 2^20 (SPLITEE_ERR_UNSUPPORTED above).
  */
 int splitee_combine(const void* H, int h_type, int64_t ldh, int64_t h_rows, const int32_t* slot, const float* weights,
                     const void* residual, int64_t ldres, void* Y, int out_type, int64_t ldy, int64_t T, int64_t k,

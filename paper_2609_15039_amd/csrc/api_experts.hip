@@ -18,7 +18,7 @@ int launch_combine(const void* H, bool h_bf16, int64_t ldh, int64_t h_rows, cons
 
 namespace {
 
-constexpr int64_t LIN_MAX_LD = int64_t(1) << 22; // a tile's rows stay within 31 bits of its first one's address
+constexpr int64_t LIN_MAX_LD = int64_t(1) << 20; // a tile's rows stay within 31 bits of its first one's address
 constexpr int64_t ROUTE_MAX_E = 1024, ROUTE_MAX_K = 64;
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -108,6 +108,8 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
     rc = check_w(W, w_type, ldw, K, in_prec);
     if (rc) return rc;
     if (lda >= LIN_MAX_LD || K >= LIN_MAX_LD || (w_type != SPLITEE_BF16_TILED && ldw >= LIN_MAX_LD)) return SPLITEE_ERR_UNSUPPORTED;
+    // gathered rows are addressed from the first one's with 31 bits
+    if (row_index && a_rows * lda * prec_elsize(in_prec) > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
     if (!pitch16(w_stride, w_type == SPLITEE_F32 ? 4 : 2)) return SPLITEE_ERR_ALIGN;
     if (rows == 0 || N == 0 || experts == 0) return SPLITEE_OK;
     if ((K > 0 && (!A || !W)) || !Y || !offsets) return SPLITEE_ERR_ARG;

@@ -20,14 +20,21 @@ struct LinArgs {
     int rows, N, K;
 };
 
-// act(z) in binary32.  expf, erff and tanhf are the device library's (a few units in the last place);
-// a NaN passes through each.
+// act(z) in binary32.  The logistic function 1 / (1 + exp(-x)) takes one hardware exponential of base 2 and one
+// hardware reciprocal (1 unit in the last place each; the product x log2 e is rounded, |x| 2^-24 of the
+// exponential, which matters where that is not small against 1: |x| below 17), a dozen instructions fewer than expf
+// and a division; tanh in the GELU's approximation is (1 + tanh u) / 2 = 1 / (1 + exp(-2 u)), without the cancellation
+// of 1 + tanh u.  A NaN passes through each.
+__device__ __forceinline__ float epi_logistic(float x)
+{
+    return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * x));
+}
 __device__ __forceinline__ float epi_act(float z, int act)
 {
     switch (act) {
-    case SPLITEE_ACT_SILU: return z / (1.0f + expf(-z));
+    case SPLITEE_ACT_SILU: return z * epi_logistic(z);
     case SPLITEE_ACT_GELU: return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-    case SPLITEE_ACT_GELU_TANH: return 0.5f * z * (1.0f + tanhf(0.79788456080286536f * (z + 0.044715f * z * z * z)));
+    case SPLITEE_ACT_GELU_TANH: return z * epi_logistic(1.59576912160573071f * (z + 0.044715f * z * z * z));
     case SPLITEE_ACT_RELU: return z < 0.0f ? 0.0f : z;
     default: return z;
     }
@@ -52,6 +59,43 @@ __device__ __forceinline__ void epi_store(const LinArgs& p, float h, int row, in
     }
 }
 
+// The activation of four z of a row, the gate's product, the residual and the store, from column n on; left:
+// columns that exist (4 and more: 16- or 8-byte accesses).
+template <bool GATED>
+__device__ __forceinline__ void epi_finish4(const LinArgs& p, float4 z, float4 up, int row, int n, int left)
+{
+    float h[4] = {z.x, z.y, z.z, z.w};
+    const float u[4] = {up.x, up.y, up.z, up.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        h[i] = epi_act(h[i], p.act);
+        if (GATED) h[i] *= u[i];
+    }
+    const int64_t at = (int64_t)row * p.ldy + n, rt = (int64_t)row * p.ldres + n;
+    if (left >= 4) {
+        if (p.out_bf16) {
+            if (p.res) {
+                const uint2 q = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p.res) + rt);
+                h[0] += __uint_as_float(q.x << 16);
+                h[1] += __uint_as_float(q.x & 0xFFFF0000u);
+                h[2] += __uint_as_float(q.y << 16);
+                h[3] += __uint_as_float(q.y & 0xFFFF0000u);
+            }
+            *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.Y) + at) = make_uint2(bf16x2_rne(h[0], h[1]), bf16x2_rne(h[2], h[3]));
+        } else {
+            if (p.res) {
+                const float4 q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.res) + rt);
+                h[0] += q.x; h[1] += q.y; h[2] += q.z; h[3] += q.w;
+            }
+            *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.Y) + at) = make_float4(h[0], h[1], h[2], h[3]);
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) epi_store(p, h[i], row, n + i);
+}
+
 // Group e's rows: begin .. end - 1, within 0 .. rows whatever offsets holds.
 __device__ __forceinline__ void group_rows(const LinArgs& p, int e, int& begin, int& end)
 {
@@ -59,26 +103,25 @@ __device__ __forceinline__ void group_rows(const LinArgs& p, int e, int& begin, 
     end = min(max(p.offsets[e + 1], begin), p.rows);
 }
 
-// The tile of BM rows at place `at` of the row tiles of all groups, counted group by group, found by the
-// whole wave: lanes take 64 groups at a time and scan their tile counts.  Returns the number of tiles of all
-// groups; e, m0 and mend (the tile's first row, the group's end) are set where at is below it.  The
-// offsets are read by every wave of a launch, a few hundred bytes from L2.
+// The group that holds row tile `at` of BM rows, the row tiles of all groups counted one group after
+// another, found by the whole wave: lanes take 64 groups at a time and scan their tile counts.  False where at
+// is past the last tile.  The offsets are read by every wave of a launch, a few hundred bytes from L2.
+struct Group {
+    int e, begin, end; // the group and its rows
+    int first, tiles;  // its first row tile and how many it has
+};
 template <int BM>
-__device__ __forceinline__ int find_tile(const LinArgs& p, int at, int& e, int& m0, int& mend)
+__device__ __forceinline__ bool find_group(const LinArgs& p, int at, Group& g)
 {
     if (!p.offsets) {
-        e = 0;
-        m0 = at * BM;
-        mend = p.rows;
-        return (p.rows + BM - 1) / BM;
+        g = Group{0, 0, p.rows, 0, (p.rows + BM - 1) / BM};
+        return at < g.tiles;
     }
     const int lane = threadIdx.x % 64;
-    int total = 0;
-    e = -1;
+    int before = 0;
     for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        const int g = e0 + lane;
         int begin = 0, end = 0;
-        if (g < p.experts) group_rows(p, g, begin, end);
+        if (e0 + lane < p.experts) group_rows(p, e0 + lane, begin, end);
         const int tiles = (end - begin + BM - 1) / BM;
         int incl = tiles;
 #pragma unroll
@@ -86,17 +129,20 @@ __device__ __forceinline__ int find_tile(const LinArgs& p, int at, int& e, int& 
             const int up = __shfl_up(incl, d, 64);
             if (lane >= d) incl += up;
         }
-        const int first = total + incl - tiles; // this group's first tile
+        const int first = before + incl - tiles;
         const uint64_t mine = __ballot(at >= first && at < first + tiles);
         if (mine) {
             const int src = __ffsll((unsigned long long)mine) - 1;
-            e = e0 + src;
-            m0 = __shfl(begin + (at - first) * BM, src, 64);
-            mend = __shfl(end, src, 64);
+            g.e = __builtin_amdgcn_readfirstlane(e0 + src);
+            g.begin = __builtin_amdgcn_readlane(begin, src);
+            g.end = __builtin_amdgcn_readlane(end, src);
+            g.first = __builtin_amdgcn_readlane(first, src);
+            g.tiles = __builtin_amdgcn_readlane(tiles, src);
+            return true;
         }
-        total += __shfl(incl, 63, 64);
+        before = __builtin_amdgcn_readlane(before + incl, 63);
     }
-    return total;
+    return false;
 }
 
 // Row of A of output row s.

@@ -1,0 +1,297 @@
+// Tiles of bfloat16 products with an epilogue on the matrix cores (gfx950), dense and by expert.
+//
+// Both operands go to LDS by 1 KB buffer loads, S stages of 64 k, in a swizzled order that the fragment reads find free
+// of bank conflicts (the tiled weight order needs none).  One barrier per K tile, before the last of its four steps:
+// the fragments of a step are read under the MFMAs of the one before, the next tile's first ones under the last step's,
+// and the freed stage is filled from there.  The epilogue takes C and bias off the accumulators where they are
+// and passes 32-row blocks through LDS, so that activation, residual and stores go row by row, four columns a lane.
+#pragma once
+#include "epilogue_dev.hpp"
+#include "gemm_dev.hpp"
+
+#include <type_traits>
+
+namespace {
+
+using splitee::LinArgs;
+
+template <int I, int BYTES>
+__device__ __forceinline__ unsigned char* lt_stage()
+{
+    __shared__ __attribute__((aligned(16))) unsigned char buf[BYTES];
+    return buf;
+}
+
+template <int N>
+using lt_int = std::integral_constant<int, N>;
+
+// 16 bytes of each lane from base + voff + soff (zeros from 2 GB on) to 1 KB of LDS at `to`
+__device__ __forceinline__ void lt_load(const void* base, uint32_t voff, int soff, unsigned char* to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(base, 0x7FFFFFFFu), (lds_ptr_t)to, 16, (int)voff, soff, 0, 0);
+}
+
+// Tile of a workgroup: which rows, which weight rows, which K tiles.
+struct LtPlan {
+    int ntiles;          // column tiles
+    int ksplit, ktps;    // splits of K and K tiles of one
+    float* part;         // partial tiles of a split K: split s at part + s * rows * ldpart, row-major; of a gated product
+    int ldpart;          // gate columns, then from ldpart / 2 up columns
+};
+
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
+struct LinTile {
+    static constexpr int NW = WGM * WGN, NT = NW * WAVE;
+    static constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32;
+    static constexpr int AB = NPL * BM * 128, SB = AB + BN * 128;
+    static constexpr int LA = NPL * BM / 8 / NW, LW = BN / 8 / NW; // 1 KB loads of a wave and stage
+    static constexpr int BNO = GATED ? BN / 2 : BN;                // output columns
+    static_assert(BN / 8 % NW == 0 && NW % 2 == 0, "loads");
+    static_assert(!GATED || TN % 2 == 0, "gate and up blocks in pairs");
+    static_assert(BM % (8 * NW) == 0, "a load lies in one plane");
+};
+
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
+__global__ void __launch_bounds__(WGM * WGN * WAVE)
+lin_tile_kernel(const LinArgs p, const LtPlan plan)
+{
+    using T = LinTile<NPL, BM, BN, WGM, WGN, S, GATED, TILED>;
+    constexpr int NW = T::NW, TM = T::TM, TN = T::TN, LA = T::LA, LW = T::LW, AB = T::AB, SB = T::SB, BNO = T::BNO;
+    constexpr int TO = GATED ? TN / 2 : TN; // column blocks of outputs of a wave
+    const int tid = threadIdx.x, lane = tid % WAVE;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
+
+    // ---- the workgroup's tile
+    splitee::Group g;
+    int L, split = 0;
+    if (p.offsets) {
+        // 16 tiles in a row on one XCD, without the total, which only the offsets know
+        constexpr int C = 16;
+        const int b = blockIdx.x, x = b % 8, i = b / 8;
+        L = (i / C) * (8 * C) + x * C + i % C;
+    } else {
+        L = (int)splitee::xcd_logical_block(blockIdx.x, gridDim.x);
+        split = L % plan.ksplit;
+        L /= plan.ksplit;
+    }
+    if (!splitee::find_group<BM>(p, L / plan.ntiles, g)) return;
+    const int in = L - g.first * plan.ntiles;
+    const int m0 = g.begin + (in % g.tiles) * BM, n0 = (in / g.tiles) * BNO;
+    const int mend = g.end;
+    const int ktiles = (p.K + BK - 1) / BK;
+    const int kt0 = split * plan.ktps, nk = min(plan.ktps, ktiles - kt0);
+
+    // ---- loads: 8 rows of 128 bytes each; lane l fills slot l % 8 of row l / 8 with the row's 16-byte chunk
+    // slot ^ ((row / 2) % 8).  Loads j = wave + NW t, so (row / 2) % 8 is the same for all of a lane's.
+    // Each is a buffer load from the tile's (of gathered rows: the matrix's) first row, its offset within the row
+    // block fixed and the K tile in the scalar offset; an offset of 2 GB and more reads zeros.
+    const int lchunk = (lane % 8) ^ ((4 * wave + lane / 16) & 7);
+    const uint16_t* const abase = reinterpret_cast<const uint16_t*>(p.A) + (p.row_index ? 0 : m0 * p.lda) + kt0 * BK;
+    constexpr int TPL = LA / NPL; // loads of a plane
+    uint32_t aoff[TPL];
+#pragma unroll
+    for (int t = 0; t < TPL; ++t) {
+        const int s = min(m0 + 8 * (wave + NW * t) + lane / 8, mend - 1); // a row past the group's: any of its rows
+        aoff[t] = (uint32_t)(((p.row_index ? splitee::a_row(p, s) : s - m0) * p.lda + lchunk * 8) * 2);
+    }
+    // LDS row block b (32 weight rows) of the tile is column block b % TN of wave column b / TN; of a gated
+    // tile the first TN / 2 are gate rows, the others the up rows of the same outputs
+    const uint16_t* const wbase = reinterpret_cast<const uint16_t*>(p.W) + (int64_t)g.e * p.w_stride;
+    const uint16_t* wb[LW]; // uniform
+    uint32_t woff[LW];
+#pragma unroll
+    for (int t = 0; t < LW; ++t) {
+        const int j = wave + NW * t, b = j / 4, wn = b / TN, jj = b % TN;
+        const bool up = jj >= TO;
+        const int c0 = n0 + 32 * (wn * TO + jj % TO); // the block's first output column
+        const int first = min(c0, p.N - 1) + (up ? p.N : 0);                   // and weight row
+        if (TILED) { // 1 KB: a 16-k step of a 32-row block, as the MFMA takes it
+            const int n = min(c0 + lane % 32, p.N - 1) + (up ? p.N : 0);
+            wb[t] = wbase + ((int64_t)(first / 32) * ktiles + kt0) * 2048;
+            woff[t] = (uint32_t)((((n / 32 - first / 32) * ktiles) * 2048 + (j % 4) * 512 + (lane / 32) * 256 + (n % 32) * 8) * 2);
+        } else {
+            const int n = min(c0 + 8 * (j % 4) + lane / 8, p.N - 1) + (up ? p.N : 0);
+            wb[t] = wbase + (int64_t)first * p.ldw + kt0 * BK;
+            woff[t] = (uint32_t)(((int64_t)(n - first) * p.ldw + lchunk * 8) * 2);
+        }
+    }
+    unsigned char* const st[4] = {lt_stage<0, SB>(), lt_stage<1, SB>(), lt_stage<(S > 2 ? 2 : 0), SB>(), lt_stage<(S > 3 ? 3 : 0), SB>()};
+    // relative K tile t into stage q: zeros past K and past the split
+    auto issue = [&](int t, auto sc) {
+        constexpr int q = decltype(sc)::value;
+        const int kleft = t < nk ? p.K - (kt0 + t) * BK : 0;
+        const uint32_t dead = lchunk * 8 < kleft ? 0u : OOB;
+        const uint32_t wdead = TILED ? (kleft > 0 ? 0u : OOB) : dead;
+#pragma unroll
+        for (int i = 0; i < LA; ++i)
+            lt_load(abase + (i / TPL) * p.pstride, aoff[i % TPL] | dead, t * (BK * 2), st[q] + (wave + NW * i) * 1024);
+#pragma unroll
+        for (int i = 0; i < LW; ++i)
+            lt_load(wb[i], woff[i] | wdead, t * (TILED ? 4096 : BK * 2), st[q] + AB + (wave + NW * i) * 1024);
+    };
+
+    f32x16_t acc[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+    // MFMA operands: lane (r, h) holds row r of a 32-row block, k = 8 h .. + 7 of the 16-k step
+    const int wm = wave / WGN, wn = wave % WGN, fr = lane % 32, fh = lane / 32;
+    const int fsw = (fr >> 1) & 7;
+    uint4 fa[2][NPL][TM], fw[2][TN];
+    auto read = [&](const unsigned char* s, int step, int to) {
+        const int off = ((2 * step + fh) ^ fsw) << 4;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+            const int b = wn * TN + j;
+            fw[to][j] = TILED ? *reinterpret_cast<const uint4*>(s + AB + b * 4096 + step * 1024 + lane * 16)
+                              : *reinterpret_cast<const uint4*>(s + AB + (32 * b + fr) * 128 + off);
+        }
+#pragma unroll
+        for (int pl = 0; pl < NPL; ++pl)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+                fa[to][pl][i] = *reinterpret_cast<const uint4*>(s + (pl * BM + 32 * (wm * TM + i) + fr) * 128 + off);
+    };
+    auto mul = [&](int from) {
+#pragma unroll
+        for (int pl = 0; pl < NPL; ++pl)
+#pragma unroll
+            for (int i = 0; i < TM; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fa[from][pl][i]), as_bf16x8(fw[from][j]), acc[i][j], 0, 0, 0);
+    };
+    constexpr int READS = TN + NPL * TM, MULS = NPL * TM * TN;
+    // K tile t in stage q, its first fragments in registers.  Steps 0 .. 2 multiply while the next step's fragments are
+    // read.  Then every wave is done with stage q, and tile t + 1 is in everywhere behind the barrier: the last step
+    // multiplies while tile t + 1's first fragments are read and tile t + S goes into stage q.
+    auto step = [&](int t, auto sc) {
+        constexpr int q = decltype(sc)::value;
+#pragma unroll
+        for (int s = 0; s < 3; ++s) {
+            read(st[q], s + 1, (s + 1) % 2);
+            mul(s % 2);
+#pragma unroll
+            for (int i = 0; i < READS; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x008, MULS / READS > 0 ? MULS / READS : 1, 0);
+            }
+            __builtin_amdgcn_sched_group_barrier(0x008, MULS, 0);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        wait_vmem<(S - 2) * (LA + LW)>();
+        __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4) | 15 | (3 << 14)); // lgkmcnt(0): the last fragments are in
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        read(st[(q + 1) % S], 0, 0);
+        issue(t + S, sc);
+        mul(1);
+#pragma unroll
+        for (int i = 0; i < READS; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < LA + LW; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, MULS, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    issue(0, lt_int<0>{});
+    issue(1, lt_int<1>{});
+    if constexpr (S > 2) issue(2, lt_int<2>{});
+    if constexpr (S > 3) issue(3, lt_int<3>{});
+    wait_vmem<(S - 1) * (LA + LW)>();
+    __builtin_amdgcn_s_barrier();
+    read(st[0], 0, 0);
+    int t = 0;
+    for (; t + S <= nk; t += S) {
+        step(t, lt_int<0>{});
+        step(t + 1, lt_int<1>{});
+        if constexpr (S > 2) step(t + 2, lt_int<2>{});
+        if constexpr (S > 3) step(t + 3, lt_int<3>{});
+    }
+    if (t < nk) step(t, lt_int<0>{});
+    if constexpr (S > 2) if (t + 1 < nk) step(t + 1, lt_int<1>{});
+    if constexpr (S > 3) if (t + 2 < nk) step(t + 2, lt_int<2>{});
+    wait_vmem<0>(); // the loads past the last tile have landed before the workgroup ends
+
+    // ---- epilogue.  Element e of lane (c, h): row 8 (e / 4) + 4 h + e % 4, column c of the 32 x 32 block.
+    const int nw0 = n0 + 32 * wn * TO;      // the wave's first output column
+    if (plan.part) {
+        float* part = plan.part + (int64_t)split * p.rows * plan.ldpart;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                const int c = nw0 + 32 * (j % TO) + fr, n = j < TO ? c : plan.ldpart / 2 + c;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = m0 + 32 * (wm * TM + i) + 8 * (e / 4) + 4 * fh + e % 4;
+                    if (row < mend && c < p.N) part[(int64_t)row * plan.ldpart + n] = acc[i][j][e];
+                }
+            }
+        return;
+    }
+    // z = acc - C + bias where the accumulators are (a lane's column is the same for all its elements of a block: one
+    // bias), every C load of a row block ahead of the first subtraction; elements outside load C[0]
+    float bias[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+        const int c = nw0 + 32 * (j % TO) + fr;
+        bias[j] = p.bias && c < p.N ? p.bias[(int64_t)g.e * p.bias_stride + (j < TO ? 0 : p.N) + c] : 0.f;
+    }
+    __syncthreads(); // every wave is done with the stages
+    constexpr int LD = 32 * TN + 8;             // of a wave's 32-row block in LDS: 4 LD is 32 banks off
+    constexpr int PER = SB / (32 * LD * 4);     // waves that a stage holds
+    static_assert(PER * S >= NW, "row blocks do not fit the stages");
+    float* zb = nullptr;
+#pragma unroll
+    for (int q = 0; q < S; ++q)
+        if (wave / PER == q) zb = reinterpret_cast<float*>(st[q]) + (wave % PER) * 32 * LD;
+    constexpr int LPR = 8 * TO, RPP = WAVE / LPR; // lanes of a row (4 columns each), rows of a pass
+    const int pr = lane / LPR, pc = lane % LPR * 4, n = nw0 + pc;
+    const int left = p.N - n;                     // columns of the lane that exist
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+        const int r0 = m0 + 32 * (wm * TM + i);
+        if (p.C) {
+            float cv[TN][16];
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = r0 + 8 * (e / 4) + 4 * fh + e % 4, c = nw0 + 32 * (j % TO) + fr;
+                    const bool in = row < mend && c < p.N;
+                    cv[j][e] = p.C[in ? (int64_t)row * p.ldc + (j < TO ? 0 : p.N) + c : 0];
+                }
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] -= cv[j][e];
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                zb[(8 * (e / 4) + 4 * fh + e % 4) * LD + 32 * j + fr] = p.bias ? acc[i][j][e] + bias[j] : acc[i][j][e];
+        // row by row, four columns a lane (a wave's own block: its LDS operations are in order)
+        const int rows_here = min(32, mend - r0);
+#pragma unroll 1
+        for (int r = pr; r < rows_here; r += RPP) {
+            if (left <= 0) break;
+            float4 z = *reinterpret_cast<const float4*>(zb + r * LD + pc), u = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (GATED) u = *reinterpret_cast<const float4*>(zb + r * LD + 32 * TO + pc);
+            splitee::epi_finish4<GATED>(p, z, u, r0 + r, n, left);
+        }
+    }
+}
+
+}  // namespace

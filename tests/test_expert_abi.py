@@ -12,7 +12,7 @@ OK, ARG, SHAPE, DTYPE, ALIGN, UNSUP, WS = 0, -1, -2, -3, -4, -5, -7
 P = 16
 F32, BF16, TILED = sp.SPLITEE_F32, sp.SPLITEE_BF16, sp.SPLITEE_BF16_TILED
 PF, PB, PX, PD = 0, 1, 2, 3
-BIG = 1 << 22
+BIG = 1 << 20
 
 
 @pytest.fixture(scope="module")
@@ -78,7 +78,7 @@ def grouped(lib, ep=None, A=P, prec=PB, lda=32, a_rows=4, index=P, offsets=P, ex
 @pytest.mark.parametrize("kw,code", COMMON + [
     (dict(rows=-1), SHAPE), (dict(a_rows=-1), SHAPE), (dict(a_rows=0), SHAPE), (dict(index=None, a_rows=3), SHAPE),
     (dict(experts=-1), SHAPE), (dict(w_stride=-8), SHAPE), (dict(w_stride=516), ALIGN), (dict(offsets=None), ARG),
-    (dict(offsets=18), ALIGN), (dict(index=18), ALIGN), (dict(rows=0), OK), (dict(experts=0), OK)])
+    (dict(a_rows=1 << 26), UNSUP), (dict(a_rows=1 << 25, prec=PF), UNSUP), (dict(offsets=18), ALIGN), (dict(index=18), ALIGN), (dict(rows=0), OK), (dict(experts=0), OK)])
 def test_grouped_validation(lib, kw, code):
     assert grouped(lib, **kw) == code
 
