@@ -59,41 +59,71 @@ __device__ __forceinline__ void epi_store(const LinArgs& p, float h, int row, in
     }
 }
 
-// The activation of four z of a row, the gate's product, the residual and the store, from column n on; left:
-// columns that exist (4 and more: 16- or 8-byte accesses).
-template <bool GATED>
-__device__ __forceinline__ void epi_finish4(const LinArgs& p, float4 z, float4 up, int row, int n, int left)
+// Four columns of a row of the residual from column n on (left of them exist), zeros without one.
+__device__ __forceinline__ float4 epi_residual4(const LinArgs& p, int row, int n, int left)
+{
+    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (!p.res) return r;
+    const int64_t at = (int64_t)row * p.ldres + n;
+    if (p.out_bf16) {
+        const uint16_t* q = reinterpret_cast<const uint16_t*>(p.res) + at;
+        if (left >= 4) {
+            const uint2 v = *reinterpret_cast<const uint2*>(q);
+            return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
+                               __uint_as_float(v.y & 0xFFFF0000u));
+        }
+        r.x = bf16_bits_to_f32(q[0]);
+        if (left > 1) r.y = bf16_bits_to_f32(q[1]);
+        if (left > 2) r.z = bf16_bits_to_f32(q[2]);
+    } else {
+        const float* q = reinterpret_cast<const float*>(p.res) + at;
+        if (left >= 4) return *reinterpret_cast<const float4*>(q);
+        r.x = q[0];
+        if (left > 1) r.y = q[1];
+        if (left > 2) r.z = q[2];
+    }
+    return r;
+}
+
+// The activation of four z of a row, the gate's product, the residual's sum and the store, from column n on; left:
+// columns that exist (4 and more: 16- or 8-byte stores).  STREAM: stores that do not stay in the L2, for results larger
+// than it (4096 x 4096 bfloat16: 2 us less).
+template <bool GATED, bool STREAM = false>
+__device__ __forceinline__ void epi_finish4(const LinArgs& p, float4 z, float4 up, float4 res, int row, int n, int left)
 {
     float h[4] = {z.x, z.y, z.z, z.w};
-    const float u[4] = {up.x, up.y, up.z, up.w};
+    const float u[4] = {up.x, up.y, up.z, up.w}, r[4] = {res.x, res.y, res.z, res.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         h[i] = epi_act(h[i], p.act);
         if (GATED) h[i] *= u[i];
+        if (p.res) h[i] += r[i]; // (-0 stays -0 without one)
     }
-    const int64_t at = (int64_t)row * p.ldy + n, rt = (int64_t)row * p.ldres + n;
-    if (left >= 4) {
-        if (p.out_bf16) {
-            if (p.res) {
-                const uint2 q = *reinterpret_cast<const uint2*>(reinterpret_cast<const uint16_t*>(p.res) + rt);
-                h[0] += __uint_as_float(q.x << 16);
-                h[1] += __uint_as_float(q.x & 0xFFFF0000u);
-                h[2] += __uint_as_float(q.y << 16);
-                h[3] += __uint_as_float(q.y & 0xFFFF0000u);
-            }
-            *reinterpret_cast<uint2*>(reinterpret_cast<uint16_t*>(p.Y) + at) = make_uint2(bf16x2_rne(h[0], h[1]), bf16x2_rne(h[2], h[3]));
+    const int64_t at = (int64_t)row * p.ldy + n;
+    if (p.out_bf16) {
+        uint16_t* y = reinterpret_cast<uint16_t*>(p.Y) + at;
+        const uint2 q = make_uint2(bf16x2_rne(h[0], h[1]), bf16x2_rne(h[2], h[3]));
+        if (left >= 4) {
+            const uint64_t v = (uint64_t)q.y << 32 | q.x;
+            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<uint64_t*>(y));
+            else *reinterpret_cast<uint64_t*>(y) = v;
         } else {
-            if (p.res) {
-                const float4 q = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p.res) + rt);
-                h[0] += q.x; h[1] += q.y; h[2] += q.z; h[3] += q.w;
-            }
-            *reinterpret_cast<float4*>(reinterpret_cast<float*>(p.Y) + at) = make_float4(h[0], h[1], h[2], h[3]);
+            y[0] = (uint16_t)q.x;
+            if (left > 1) y[1] = (uint16_t)(q.x >> 16);
+            if (left > 2) y[2] = (uint16_t)q.y;
         }
-        return;
+    } else {
+        float* y = reinterpret_cast<float*>(p.Y) + at;
+        if (left >= 4) {
+            const f32x4_t v = {h[0], h[1], h[2], h[3]};
+            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<f32x4_t*>(y));
+            else *reinterpret_cast<f32x4_t*>(y) = v;
+        } else {
+            y[0] = h[0];
+            if (left > 1) y[1] = h[1];
+            if (left > 2) y[2] = h[2];
+        }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (i < left) epi_store(p, h[i], row, n + i);
 }
 
 // Group e's rows: begin .. end - 1, within 0 .. rows whatever offsets holds.

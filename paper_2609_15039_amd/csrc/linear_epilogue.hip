@@ -88,7 +88,8 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinArgs p, const float*
             if (n + i < p.N) z[h][i] = splitee::epi_z(p, z[h][i], 0, row, h * p.N + n + i);
     }
     splitee::epi_finish4<GATED>(p, make_float4(z[0][0], z[0][1], z[0][2], z[0][3]),
-                                make_float4(z[GATED][0], z[GATED][1], z[GATED][2], z[GATED][3]), row, n, p.N - n);
+                                make_float4(z[GATED][0], z[GATED][1], z[GATED][2], z[GATED][3]),
+                                splitee::epi_residual4(p, row, n, p.N - n), row, n, p.N - n);
 }
 
 }  // namespace
@@ -113,7 +114,7 @@ LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t
     LinPlan best{};
     best.cost = 1e30;
     for (int bm = 8; bm <= 16; bm *= 2) {
-        LinPlan p{LinPlan::ROWS, bm, 2, 4, 1, (int)kt, 0.0};
+        LinPlan p{LinPlan::ROWS, bm, 2, 4, 1, (int)kt, false, 0.0};
         auto wgs = [&]() { const int bno = 16 * p.tn / (gated ? 2 : 1); return strips(bm) * ((N + bno - 1) / bno); };
         if (!gated && wgs() < 256) p.tn = 1; // 16 columns each: more CUs at work
         // eight waves where K is long and their stages leave room for two workgroups, or there are few
@@ -121,16 +122,25 @@ LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t
         p.cost = 5 + std::max(wgs() * kt * 5.5e-4 * p.tn / 2, (double)((kt + p.nw - 1) / p.nw) * 0.5);
         if (p.cost < best.cost) best = p;
     }
-    for (int big = 0; big < 2; ++big) {
-        const int bm = big ? 128 : 64, bno = (big ? 256 : 128) / (gated ? 2 : 1);
-        const double tiles = strips(bm) * ((N + bno - 1) / bno);
-        const int most = dense ? (int)std::min<int64_t>(8, std::max<int64_t>(1, kt / 4)) : 1;
+    // microseconds of a K tile, alone on a CU (64 x 128) or with as many as fit, and of all else
+    struct Tile { LinPlan::Kind kind; int bm, bn, slots; double alone, full, fixed; bool split, halves; };
+    const Tile tiles[] = {
+        {LinPlan::TILE64, 64, 128, 512, npl == 1 ? 0.30 : 0.90, npl == 1 ? 0.80 : 1.40, 6, true, false},
+        {LinPlan::TILE128, 128, 256, 256, npl == 1 ? 1.0 : 2.15, npl == 1 ? 1.0 : 2.15, 8, true, npl == 3},
+        {LinPlan::TILE256, 256, 256, 256, 1.5, 1.5, 12, false, true}};
+    for (const Tile& t : tiles) {
+        if (t.kind == LinPlan::TILE256 && npl != 1) continue;
+        const int bno = t.bn / (gated ? 2 : 1);
+        const double n = strips(t.bm) * ((N + bno - 1) / bno);
+        const int most = dense && t.split ? (int)std::min<int64_t>(8, std::max<int64_t>(1, kt / 4)) : 1;
         for (int ks = 1; ks <= most; ++ks) {
-            LinPlan p{big ? LinPlan::TILE128 : LinPlan::TILE64, 0, 0, 0, ks, (int)((kt + ks - 1) / ks), 0.0};
+            LinPlan p{t.kind, 0, 0, 0, ks, (int)((kt + ks - 1) / ks), false, 0.0};
             if ((int64_t)(ks - 1) * p.ktps >= kt) continue; // a split without K tiles
-            const double wgs = tiles * ks;
-            const double per = big ? (npl == 1 ? 1.0 : 2.15) : wgs <= 256 ? (npl == 1 ? 0.30 : 0.90) : (npl == 1 ? 0.70 : 1.06);
-            p.cost = (big ? 8 : 6) + std::ceil(wgs / (big ? 256 : 512)) * p.ktps * per;
+            const double wgs = n * ks, rounds = std::floor(wgs / t.slots);
+            const double round = p.ktps * (t.alone + (t.full - t.alone) * std::min(1.0, std::max(0.0, (wgs - 256) / 256)));
+            const double rest = wgs - rounds * t.slots;
+            p.halve = dense && t.halves && ks == 1 && rest > 0 && rest <= t.slots / 2;
+            p.cost = t.fixed + rounds * round + (rest == 0 ? 0 : p.halve ? 0.62 * round : !dense && rounds >= 2 ? rest / t.slots * round : round);
             if (ks > 1) p.cost += 4 + ks * rows * part_ld(N, gated) * 8.0 / 4e6;
             if (p.cost < best.cost) best = p;
         }

@@ -6,9 +6,10 @@ namespace splitee_host {
 
 // kind: few rows (BM rows, TN 16-row weight blocks, NW waves) or a tile (BM x BN, K split into ksplit)
 struct LinPlan {
-    enum Kind { ROWS, TILE64, TILE128 } kind;
+    enum Kind { ROWS, TILE64, TILE128, TILE256 } kind;
     int bm, tn, nw; // ROWS
     int ksplit, ktps;
+    bool halve;     // the tiles of the last, partly filled round in two halves each
     double cost;    // microseconds
 };
 

@@ -31,19 +31,29 @@ __device__ __forceinline__ void lt_load(const void* base, uint32_t voff, int sof
     __builtin_amdgcn_raw_ptr_buffer_load_lds(make_rsrc(base, 0x7FFFFFFFu), (lds_ptr_t)to, 16, (int)voff, soff, 0, 0);
 }
 
+// Barrier of the workgroup for its LDS alone: stores to memory may still be on their way.
+__device__ __forceinline__ void lt_barrier()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 // Tile of a workgroup: which rows, which weight rows, which K tiles.
 struct LtPlan {
     int ntiles;          // column tiles
     int ksplit, ktps;    // splits of K and K tiles of one
     float* part;         // partial tiles of a split K: split s at part + s * rows * ldpart, row-major; of a gated product
     int ldpart;          // gate columns, then from ldpart / 2 up columns
+    int nbig;            // HALF, dense: tiles that are not halved
 };
 
 template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
 struct LinTile {
     static constexpr int NW = WGM * WGN, NT = NW * WAVE;
     static constexpr int TM = BM / WGM / 32, TN = BN / WGN / 32;
-    static constexpr int AB = NPL * BM * 128, SB = AB + BN * 128;
+    static constexpr int AB = NPL * BM * 128;
+    static constexpr int SB = AB + BN * 128;
     static constexpr int LA = NPL * BM / 8 / NW, LW = BN / 8 / NW; // 1 KB loads of a wave and stage
     static constexpr int BNO = GATED ? BN / 2 : BN;                // output columns
     static_assert(BN / 8 % NW == 0 && NW % 2 == 0, "loads");
@@ -51,33 +61,18 @@ struct LinTile {
     static_assert(BM % (8 * NW) == 0, "a load lies in one plane");
 };
 
-template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
-__global__ void __launch_bounds__(WGM * WGN * WAVE)
-lin_tile_kernel(const LinArgs p, const LtPlan plan)
+// Rows m0 .. mend - 1 (at most BM of them) and the weight rows from output column n0 on.  SB: bytes of a stage, those
+// of the largest tile that the kernel has.
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED, int SB>
+__device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, const splitee::Group& g, int m0, int n0, int mend,
+                                         int split)
 {
     using T = LinTile<NPL, BM, BN, WGM, WGN, S, GATED, TILED>;
-    constexpr int NW = T::NW, TM = T::TM, TN = T::TN, LA = T::LA, LW = T::LW, AB = T::AB, SB = T::SB, BNO = T::BNO;
+    constexpr int NW = T::NW, TM = T::TM, TN = T::TN, LA = T::LA, LW = T::LW, AB = T::AB;
     constexpr int TO = GATED ? TN / 2 : TN; // column blocks of outputs of a wave
+    static_assert(T::SB <= SB, "stage");
     const int tid = threadIdx.x, lane = tid % WAVE;
     const int wave = __builtin_amdgcn_readfirstlane(tid / WAVE);
-
-    // ---- the workgroup's tile
-    splitee::Group g;
-    int L, split = 0;
-    if (p.offsets) {
-        // 16 tiles in a row on one XCD, without the total, which only the offsets know
-        constexpr int C = 16;
-        const int b = blockIdx.x, x = b % 8, i = b / 8;
-        L = (i / C) * (8 * C) + x * C + i % C;
-    } else {
-        L = (int)splitee::xcd_logical_block(blockIdx.x, gridDim.x);
-        split = L % plan.ksplit;
-        L /= plan.ksplit;
-    }
-    if (!splitee::find_group<BM>(p, L / plan.ntiles, g)) return;
-    const int in = L - g.first * plan.ntiles;
-    const int m0 = g.begin + (in % g.tiles) * BM, n0 = (in / g.tiles) * BNO;
-    const int mend = g.end;
     const int ktiles = (p.K + BK - 1) / BK;
     const int kt0 = split * plan.ktps, nk = min(plan.ktps, ktiles - kt0);
 
@@ -115,19 +110,17 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
             woff[t] = (uint32_t)(((int64_t)(n - first) * p.ldw + lchunk * 8) * 2);
         }
     }
-    unsigned char* const st[4] = {lt_stage<0, SB>(), lt_stage<1, SB>(), lt_stage<(S > 2 ? 2 : 0), SB>(), lt_stage<(S > 3 ? 3 : 0), SB>()};
-    // relative K tile t into stage q: zeros past K and past the split
-    auto issue = [&](int t, auto sc) {
-        constexpr int q = decltype(sc)::value;
+    unsigned char* const st[3] = {lt_stage<0, SB>(), lt_stage<1, SB>(), lt_stage<(S > 2 ? 2 : 0), SB>()};
+    static_assert(S == 2 || S == 3, "stages");
+    // relative K tile t to the stage at `to`: zeros past K and past the split
+    auto issue = [&](int t, unsigned char* to) {
         const int kleft = t < nk ? p.K - (kt0 + t) * BK : 0;
-        const uint32_t dead = lchunk * 8 < kleft ? 0u : OOB;
-        const uint32_t wdead = TILED ? (kleft > 0 ? 0u : OOB) : dead;
+        const uint32_t dead = lchunk * 8 < kleft ? 0u : OOB, wdead = TILED ? (kleft > 0 ? 0u : OOB) : dead;
 #pragma unroll
         for (int i = 0; i < LA; ++i)
-            lt_load(abase + (i / TPL) * p.pstride, aoff[i % TPL] | dead, t * (BK * 2), st[q] + (wave + NW * i) * 1024);
+            lt_load(abase + (i / TPL) * p.pstride, aoff[i % TPL] | dead, t * (BK * 2), to + (wave + NW * i) * 1024);
 #pragma unroll
-        for (int i = 0; i < LW; ++i)
-            lt_load(wb[i], woff[i] | wdead, t * (TILED ? 4096 : BK * 2), st[q] + AB + (wave + NW * i) * 1024);
+        for (int i = 0; i < LW; ++i) lt_load(wb[i], woff[i] | wdead, t * (TILED ? 4096 : BK * 2), to + AB + (wave + NW * i) * 1024);
     };
 
     f32x16_t acc[TM][TN];
@@ -142,19 +135,20 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
     const int wm = wave / WGN, wn = wave % WGN, fr = lane % 32, fh = lane / 32;
     const int fsw = (fr >> 1) & 7;
     uint4 fa[2][NPL][TM], fw[2][TN];
-    auto read = [&](const unsigned char* s, int step, int to) {
+    auto read = [&](const unsigned char* sa, int step, int to) {
+        const unsigned char* const sw = sa + AB;
         const int off = ((2 * step + fh) ^ fsw) << 4;
 #pragma unroll
         for (int j = 0; j < TN; ++j) {
             const int b = wn * TN + j;
-            fw[to][j] = TILED ? *reinterpret_cast<const uint4*>(s + AB + b * 4096 + step * 1024 + lane * 16)
-                              : *reinterpret_cast<const uint4*>(s + AB + (32 * b + fr) * 128 + off);
+            fw[to][j] = TILED ? *reinterpret_cast<const uint4*>(sw + b * 4096 + step * 1024 + lane * 16)
+                              : *reinterpret_cast<const uint4*>(sw + (32 * b + fr) * 128 + off);
         }
 #pragma unroll
         for (int pl = 0; pl < NPL; ++pl)
 #pragma unroll
             for (int i = 0; i < TM; ++i)
-                fa[to][pl][i] = *reinterpret_cast<const uint4*>(s + (pl * BM + 32 * (wm * TM + i) + fr) * 128 + off);
+                fa[to][pl][i] = *reinterpret_cast<const uint4*>(sa + (pl * BM + 32 * (wm * TM + i) + fr) * 128 + off);
     };
     auto mul = [&](int from) {
 #pragma unroll
@@ -166,14 +160,14 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(fa[from][pl][i]), as_bf16x8(fw[from][j]), acc[i][j], 0, 0, 0);
     };
     constexpr int READS = TN + NPL * TM, MULS = NPL * TM * TN;
-    // K tile t in stage q, its first fragments in registers.  Steps 0 .. 2 multiply while the next step's fragments are
-    // read.  Then every wave is done with stage q, and tile t + 1 is in everywhere behind the barrier: the last step
-    // multiplies while tile t + 1's first fragments are read and tile t + S goes into stage q.
-    auto step = [&](int t, auto sc) {
-        constexpr int q = decltype(sc)::value;
+    // K tile t, its first fragments in registers.  Steps 0 .. 2 multiply while the next step's fragments are read.  Then
+    // every wave is done with the tile, and tile t + 1 is in everywhere behind the barrier: the last step multiplies
+    // while tile t + 1's first fragments are read and the loads into the freed LDS begin.  c: t modulo a turn.
+    auto step = [&](int t, auto cc) {
+        constexpr int c = decltype(cc)::value;
 #pragma unroll
         for (int s = 0; s < 3; ++s) {
-            read(st[q], s + 1, (s + 1) % 2);
+            read(st[c], s + 1, (s + 1) % 2);
             mul(s % 2);
 #pragma unroll
             for (int i = 0; i < READS; ++i) {
@@ -187,8 +181,8 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
         __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4) | 15 | (3 << 14)); // lgkmcnt(0): the last fragments are in
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        read(st[(q + 1) % S], 0, 0);
-        issue(t + S, sc);
+        read(st[(c + 1) % S], 0, 0);
+        issue(t + S, st[c]);
         mul(1);
 #pragma unroll
         for (int i = 0; i < READS; ++i) {
@@ -204,10 +198,8 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    issue(0, lt_int<0>{});
-    issue(1, lt_int<1>{});
-    if constexpr (S > 2) issue(2, lt_int<2>{});
-    if constexpr (S > 3) issue(3, lt_int<3>{});
+#pragma unroll
+    for (int q = 0; q < S; ++q) issue(q, st[q]);
     wait_vmem<(S - 1) * (LA + LW)>();
     __builtin_amdgcn_s_barrier();
     read(st[0], 0, 0);
@@ -216,11 +208,9 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
         step(t, lt_int<0>{});
         step(t + 1, lt_int<1>{});
         if constexpr (S > 2) step(t + 2, lt_int<2>{});
-        if constexpr (S > 3) step(t + 3, lt_int<3>{});
     }
     if (t < nk) step(t, lt_int<0>{});
     if constexpr (S > 2) if (t + 1 < nk) step(t + 1, lt_int<1>{});
-    if constexpr (S > 3) if (t + 2 < nk) step(t + 2, lt_int<2>{});
     wait_vmem<0>(); // the loads past the last tile have landed before the workgroup ends
 
     // ---- epilogue.  Element e of lane (c, h): row 8 (e / 4) + 4 h + e % 4, column c of the 32 x 32 block.
@@ -241,57 +231,118 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
         return;
     }
     // z = acc - C + bias where the accumulators are (a lane's column is the same for all its elements of a block: one
-    // bias), every C load of a row block ahead of the first subtraction; elements outside load C[0]
+    // bias)
     float bias[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
         const int c = nw0 + 32 * (j % TO) + fr;
         bias[j] = p.bias && c < p.N ? p.bias[(int64_t)g.e * p.bias_stride + (j < TO ? 0 : p.N) + c] : 0.f;
     }
-    __syncthreads(); // every wave is done with the stages
-    constexpr int LD = 32 * TN + 8;             // of a wave's 32-row block in LDS: 4 LD is 32 banks off
-    constexpr int PER = SB / (32 * LD * 4);     // waves that a stage holds
-    static_assert(PER * S >= NW, "row blocks do not fit the stages");
+    // a 32-row block in LDS: columns of every second four rows 32 over, into the other half of the banks
+    static_assert(32 * BN * 4 <= SB && WGM <= S, "a row block of each wave row fits a stage");
+    auto z_at = [&](int r, int c) { return r * BN + (c ^ ((r >> 2 & 1) << 5)); };
     float* zb = nullptr;
 #pragma unroll
-    for (int q = 0; q < S; ++q)
-        if (wave / PER == q) zb = reinterpret_cast<float*>(st[q]) + (wave % PER) * 32 * LD;
-    constexpr int LPR = 8 * TO, RPP = WAVE / LPR; // lanes of a row (4 columns each), rows of a pass
-    const int pr = lane / LPR, pc = lane % LPR * 4, n = nw0 + pc;
-    const int left = p.N - n;                     // columns of the lane that exist
+    for (int q = 0; q < WGM; ++q)
+        if (wm == q) zb = reinterpret_cast<float*>(st[q]);
+    // the activation and the stores take rows of the wave row's block, 4 columns a lane: up to 1 KB in a row
+    constexpr int BNO = T::BNO, LPR = BNO / 4, RPP = WAVE / LPR, RSTEP = WGN * RPP;
+    static_assert(LPR <= WAVE, "columns of a row");
+    const int pr = wn * RPP + lane / LPR, pc = lane % LPR * 4, n = n0 + pc;
+    const int left = p.N - n; // columns of the lane that exist
+    // C of up to two row blocks of the wave ahead of both; elements outside load C[0].  (To wait for a load is to wait
+    // for every store before it too.)
+    constexpr int CB = TM < 2 ? TM : 2;
+    float cv[CB][TN][16];
+    auto load_c = [&](int i, int to) {
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int row = m0 + 32 * (wm * TM + i) + 8 * (e / 4) + 4 * fh + e % 4, c = nw0 + 32 * (j % TO) + fr;
+                cv[to][j][e] = p.C[row < mend && c < p.N ? (int64_t)row * p.ldc + (j < TO ? 0 : p.N) + c : 0];
+            }
+    };
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
         const int r0 = m0 + 32 * (wm * TM + i);
         if (p.C) {
-            float cv[TN][16];
+            if (i % CB == 0) {
+#pragma unroll
+                for (int k = 0; k < CB; ++k) load_c(i + k, k);
+            }
 #pragma unroll
             for (int j = 0; j < TN; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int row = r0 + 8 * (e / 4) + 4 * fh + e % 4, c = nw0 + 32 * (j % TO) + fr;
-                    const bool in = row < mend && c < p.N;
-                    cv[j][e] = p.C[in ? (int64_t)row * p.ldc + (j < TO ? 0 : p.N) + c : 0];
-                }
-#pragma unroll
-            for (int j = 0; j < TN; ++j)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[i][j][e] -= cv[j][e];
+                for (int e = 0; e < 16; ++e) acc[i][j][e] -= cv[i % CB][j][e];
         }
+        lt_barrier(); // every wave is done with the stages, or with the row block before
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-                zb[(8 * (e / 4) + 4 * fh + e % 4) * LD + 32 * j + fr] = p.bias ? acc[i][j][e] + bias[j] : acc[i][j][e];
-        // row by row, four columns a lane (a wave's own block: its LDS operations are in order)
-        const int rows_here = min(32, mend - r0);
+                zb[z_at(8 * (e / 4) + 4 * fh + e % 4, (j < TO ? 0 : BNO) + 32 * (wn * TO + j % TO) + fr)] =
+                    p.bias ? acc[i][j][e] + bias[j] : acc[i][j][e];
+        lt_barrier();
+        const int rows_here = left > 0 ? min(32, mend - r0) : 0;
+        auto gate = [&](int r) { return *reinterpret_cast<const float4*>(zb + z_at(r, pc)); };
+        auto up = [&](int r) { return GATED ? *reinterpret_cast<const float4*>(zb + z_at(r, BNO + pc)) : make_float4(0.f, 0.f, 0.f, 0.f); };
+        if (!p.res) { // stores alone: with loads in the loop, each row would wait for the store before
 #pragma unroll 1
-        for (int r = pr; r < rows_here; r += RPP) {
-            if (left <= 0) break;
-            float4 z = *reinterpret_cast<const float4*>(zb + r * LD + pc), u = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (GATED) u = *reinterpret_cast<const float4*>(zb + r * LD + 32 * TO + pc);
-            splitee::epi_finish4<GATED>(p, z, u, r0 + r, n, left);
+            for (int r = pr; r < rows_here; r += RSTEP)
+                splitee::epi_finish4<GATED, true>(p, gate(r), up(r), make_float4(0.f, 0.f, 0.f, 0.f), r0 + r, n, left);
+        } else if (pr < rows_here) {
+            float4 res = splitee::epi_residual4(p, r0 + pr, n, left);
+#pragma unroll 1
+            for (int r = pr; r < rows_here; r += RSTEP) {
+                const float4 next = splitee::epi_residual4(p, r0 + min(r + RSTEP, rows_here - 1), n, left);
+                splitee::epi_finish4<GATED, true>(p, gate(r), up(r), res, r0 + r, n, left);
+                res = next;
+            }
         }
     }
+}
+
+// HALF: the tiles from plan.nbig on are computed as two of BM / 2 rows, and so is a tile with at most BM / 2 rows:
+// the last, partly filled round of workgroups then takes little more than half a round's time.
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED, bool HALF>
+__global__ void __launch_bounds__(WGM * WGN * WAVE)
+lin_tile_kernel(const LinArgs p, const LtPlan plan)
+{
+    using T = LinTile<NPL, BM, BN, WGM, WGN, S, GATED, TILED>;
+    int L, split = 0, half = 0;
+    if (p.offsets) {
+        // 16 tiles in a row on one XCD, without the total, which only the offsets know
+        constexpr int C = 16;
+        const int b = blockIdx.x, x = b % 8, i = b / 8;
+        L = (i / C) * (8 * C) + x * C + i % C;
+    } else if (HALF && (int)blockIdx.x >= plan.nbig) {
+        const int h = (int)splitee::xcd_logical_block(blockIdx.x - plan.nbig, gridDim.x - plan.nbig);
+        L = plan.nbig + h / 2;
+        half = 1 + h % 2;
+    } else {
+        L = (int)splitee::xcd_logical_block(blockIdx.x, HALF ? (uint32_t)plan.nbig : gridDim.x);
+        split = L % plan.ksplit;
+        L /= plan.ksplit;
+    }
+    splitee::Group g;
+    if (!splitee::find_group<BM>(p, L / plan.ntiles, g)) return;
+    const int in = L - g.first * plan.ntiles;
+    // eight row tiles times all columns at a time: the 32 tiles that an XCD has at once then share 8 + 4 operand tiles
+    // (128 x 256 tiles of 4096 x 4096 x 2560: 89 -> 86 us)
+    const int m1 = in / (8 * plan.ntiles) * 8, ms = min(8, g.tiles - m1), rest = in - m1 * plan.ntiles;
+    int m0 = g.begin + (m1 + rest % ms) * BM, mend = min(m0 + BM, g.end);
+    const int n0 = rest / ms * T::BNO;
+    if constexpr (HALF) {
+        if (half == 1) mend = min(mend, m0 + BM / 2);
+        if (half == 2) m0 += BM / 2;
+        if (m0 >= mend) return;
+        if (mend - m0 <= BM / 2) {
+            lin_tile<NPL, BM / 2, BN, WGM, WGN, S, GATED, TILED, T::SB>(p, plan, g, m0, n0, mend, split);
+            return;
+        }
+    }
+    lin_tile<NPL, BM, BN, WGM, WGN, S, GATED, TILED, T::SB>(p, plan, g, m0, n0, mend, split);
 }
 
 }  // namespace

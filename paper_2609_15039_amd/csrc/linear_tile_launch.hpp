@@ -5,29 +5,39 @@
 
 namespace {
 
-template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool HALF, bool GATED, bool TILED>
 int tile_run(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, hipStream_t s)
 {
     using T = LinTile<NPL, BM, BN, WGM, WGN, S, GATED, TILED>;
     const int64_t nt = (p.N + T::BNO - 1) / T::BNO;
     const int64_t strips = p.offsets ? p.rows / BM + (int64_t)p.experts : (p.rows + BM - 1) / BM;
-    const int64_t wgs = p.offsets ? (strips * nt + 127) / 128 * 128 : strips * nt * plan.ksplit; // (by expert: the 8 x 16 order)
+    const int64_t tiles = strips * nt, nbig = HALF && plan.halve ? tiles / 256 * 256 : tiles;
+    const int64_t wgs = p.offsets ? (tiles + 127) / 128 * 128 // (by expert: the 8 x 16 order)
+                                  : (nbig + 2 * (tiles - nbig)) * plan.ksplit;
     if (wgs > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
-    const LtPlan lt{(int)nt, plan.ksplit, plan.ktps, part, (int)splitee_host::part_ld(p.N, GATED)};
-    hipLaunchKernelGGL((lin_tile_kernel<NPL, BM, BN, WGM, WGN, S, GATED, TILED>), dim3((unsigned)wgs), dim3(T::NT), 0, s, p, lt);
+    const LtPlan lt{(int)nt, plan.ksplit, plan.ktps, part, (int)splitee_host::part_ld(p.N, GATED), (int)nbig};
+    hipLaunchKernelGGL((lin_tile_kernel<NPL, BM, BN, WGM, WGN, S, GATED, TILED, HALF>), dim3((unsigned)wgs), dim3(T::NT), 0, s, p, lt);
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
 }
 
-// Stages: of 64 x 128 tiles as many as let two workgroups share a CU's 160 KB, of 128 x 256 as many as fit.
+template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool HALF, bool TILED>
+int tile_gated(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, hipStream_t s)
+{
+    return p.gated ? tile_run<NPL, BM, BN, WGM, WGN, S, HALF, true, TILED>(p, plan, part, s)
+                   : tile_run<NPL, BM, BN, WGM, WGN, S, HALF, false, TILED>(p, plan, part, s);
+}
+
+// Stages: of 64 x 128 tiles as many as let two workgroups share a CU's 160 KB, of the others as many as fit.
 template <int NPL, bool TILED>
 int tile_size(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, hipStream_t s)
 {
+    using splitee_host::LinPlan;
     constexpr int S = NPL == 1 ? 3 : 2;
-    if (plan.kind == splitee_host::LinPlan::TILE64)
-        return p.gated ? tile_run<NPL, 64, 128, 2, 2, S, true, TILED>(p, plan, part, s)
-                       : tile_run<NPL, 64, 128, 2, 2, S, false, TILED>(p, plan, part, s);
-    return p.gated ? tile_run<NPL, 128, 256, 2, 4, S, true, TILED>(p, plan, part, s)
-                   : tile_run<NPL, 128, 256, 2, 4, S, false, TILED>(p, plan, part, s);
+    if (plan.kind == LinPlan::TILE64) return tile_gated<NPL, 64, 128, 2, 2, S, false, TILED>(p, plan, part, s);
+    if constexpr (NPL == 1)
+        if (plan.kind == LinPlan::TILE256) return tile_gated<1, 256, 256, 2, 4, 2, true, TILED>(p, plan, part, s);
+    if (NPL == 3 && plan.ksplit == 1) return tile_gated<NPL, 128, 256, 2, 4, S, NPL == 3, TILED>(p, plan, part, s);
+    return tile_gated<NPL, 128, 256, 2, 4, S, false, TILED>(p, plan, part, s);
 }
 
 }  // namespace
