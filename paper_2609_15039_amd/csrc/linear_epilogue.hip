@@ -11,60 +11,6 @@ namespace {
 
 using splitee::LinArgs;
 
-constexpr int LS_T = 16;  // rows and columns of a tile
-constexpr int LS_K = 32;  // k of one stage
-
-__device__ __forceinline__ float ls_w(const LinArgs& p, int w_type, int e, int n, int k)
-{
-    const int64_t base = (int64_t)e * p.w_stride;
-    if (w_type == SPLITEE_F32) return reinterpret_cast<const float*>(p.W)[base + (int64_t)n * p.ldw + k];
-    const uint16_t* w = reinterpret_cast<const uint16_t*>(p.W) + base;
-    if (w_type == SPLITEE_BF16) return splitee::bf16_bits_to_f32(w[(int64_t)n * p.ldw + k]);
-    const int64_t kt = (p.K + 63) / 64;
-    return splitee::bf16_bits_to_f32(
-        w[((((int64_t)(n / 32) * kt + k / 64) * 4 + (k % 64) / 16) * 64 + ((k % 16) / 8) * 32 + n % 32) * 8 + k % 8]);
-}
-
-__device__ __forceinline__ float ls_a(const LinArgs& p, int prec, int64_t row, int k)
-{
-    const int64_t i = row * p.lda + k;
-    if (prec == SPLITEE_PREC_F32) return reinterpret_cast<const float*>(p.A)[i];
-    const uint16_t* a = reinterpret_cast<const uint16_t*>(p.A);
-    float x = splitee::bf16_bits_to_f32(a[i]);
-    if (prec == SPLITEE_PREC_BF16X3) // exact: the planes sum to a binary32 value
-        x = (x + splitee::bf16_bits_to_f32(a[p.pstride + i])) + splitee::bf16_bits_to_f32(a[2 * p.pstride + i]);
-    return x;
-}
-
-// One thread per output, operands through LDS as binary32.
-__global__ void __launch_bounds__(LS_T * LS_T) linear_simple_kernel(LinArgs p, int prec, int w_type)
-{
-    __shared__ float sa[LS_T][LS_K + 1], sw[2][LS_T][LS_K + 1];
-    splitee::Group g;
-    if (!splitee::find_group<LS_T>(p, blockIdx.y, g)) return;
-    const int e = g.e, m0 = g.begin + ((int)blockIdx.y - g.first) * LS_T, mend = g.end;
-    const int n0 = blockIdx.x * LS_T, tid = threadIdx.x, r = tid / LS_T, c = tid % LS_T;
-    const int halves = p.gated ? 2 : 1;
-    float acc[2] = {0.f, 0.f};
-    for (int k0 = 0; k0 < p.K; k0 += LS_K) {
-        for (int i = tid; i < LS_T * LS_K; i += LS_T * LS_T) {
-            const int ir = i / LS_K, k = k0 + i % LS_K;
-            sa[ir][i % LS_K] = m0 + ir < mend && k < p.K ? ls_a(p, prec, splitee::a_row(p, m0 + ir), k) : 0.f;
-            for (int h = 0; h < halves; ++h)
-                sw[h][ir][i % LS_K] = n0 + ir < p.N && k < p.K ? ls_w(p, w_type, e, n0 + ir + h * p.N, k) : 0.f;
-        }
-        __syncthreads();
-        for (int k = 0; k < LS_K; ++k)
-            for (int h = 0; h < halves; ++h) acc[h] = fmaf(sa[r][k], sw[h][c][k], acc[h]);
-        __syncthreads();
-    }
-    const int row = m0 + r, n = n0 + c;
-    if (row >= mend || n >= p.N) return;
-    float h = splitee::epi_act(splitee::epi_z(p, acc[0], e, row, n), p.act);
-    if (p.gated) h *= splitee::epi_z(p, acc[1], e, row, n + p.N);
-    splitee::epi_store(p, h, row, n);
-}
-
 // The partial products of a split K, added in split order, and the epilogue: four columns a thread.
 template <bool GATED>
 __global__ void __launch_bounds__(256) linear_sum_kernel(LinArgs p, const float* __restrict__ part, int ksplit, int ldpart)
@@ -126,10 +72,10 @@ LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t
     struct Tile { LinPlan::Kind kind; int bm, bn, slots; double alone, full, fixed; bool split, halves; };
     const Tile tiles[] = {
         {LinPlan::TILE64, 64, 128, 512, npl == 1 ? 0.30 : 0.90, npl == 1 ? 0.80 : 1.40, 6, true, false},
-        {LinPlan::TILE128, 128, 256, 256, npl == 1 ? 1.0 : 2.15, npl == 1 ? 1.0 : 2.15, 8, true, npl == 3},
+        {LinPlan::TILE128, 128, 256, 256, npl == 1 ? 1.0 : 2.15, npl == 1 ? 1.0 : 2.15, 8, true, true},
         {LinPlan::TILE256, 256, 256, 256, 1.5, 1.5, 12, false, true}};
     for (const Tile& t : tiles) {
-        if (t.kind == LinPlan::TILE256 && npl != 1) continue;
+        if (t.kind == LinPlan::TILE256 && (npl != 1 || !dense)) continue;
         const int bno = t.bn / (gated ? 2 : 1);
         const double n = strips(t.bm) * ((N + bno - 1) / bno);
         const int most = dense && t.split ? (int)std::min<int64_t>(8, std::max<int64_t>(1, kt / 4)) : 1;
@@ -148,37 +94,74 @@ LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t
     return best;
 }
 
+namespace {
+
+// Dense binary32: the GEMM's partials (behind its counters, which it does not use), then the product, in the layout
+// of one split; gate and up are two GEMMs where the up rows' columns would not be 16-byte aligned.
+struct F32Dense {
+    int64_t n;           // columns of a GEMM
+    int halves;          // GEMMs
+    int64_t ld;
+    size_t gemm, bytes;  // of the GEMM's part and of all
+};
+F32Dense f32_dense(int64_t M, int64_t N, int64_t K, int gated)
+{
+    F32Dense d{};
+    d.halves = gated && N % 4 != 0 ? 2 : 1;
+    d.n = gated && d.halves == 1 ? 2 * N : N;
+    d.ld = part_ld(N, gated);
+    d.gemm = (splitee::WS_COUNTER_BYTES + f32_gemm_workspace_bytes(M, d.n, K) + 255) / 256 * 256;
+    d.bytes = d.gemm + (size_t)M * d.ld * 4;
+    return d;
+}
+
+int launch_sum(const LinArgs& p, const float* part, int ksplit, hipStream_t s)
+{
+    const int64_t quads = (int64_t)p.rows * ((p.N + 3) / 4);
+    const int ld = (int)part_ld(p.N, p.gated);
+    if ((quads + 255) / 256 > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
+    const dim3 grid((unsigned)((quads + 255) / 256));
+    if (p.gated) hipLaunchKernelGGL(linear_sum_kernel<true>, grid, dim3(256), 0, s, p, part, ksplit, ld);
+    else hipLaunchKernelGGL(linear_sum_kernel<false>, grid, dim3(256), 0, s, p, part, ksplit, ld);
+    return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
+}
+
+int launch_dense_f32(const LinArgs& p, int w_type, void* ws, hipStream_t s)
+{
+    const F32Dense d = f32_dense(p.rows, p.N, p.K, p.gated);
+    const float* A = reinterpret_cast<const float*>(p.A);
+    if (!p.gated && !p.bias && !p.res && p.act == SPLITEE_ACT_NONE && !p.out_bf16) // the unmask is the GEMM's own
+        return launch_gemm_f32(A, p.lda, p.W, w_type, p.ldw, p.C, p.ldc, reinterpret_cast<float*>(p.Y), p.ldy, p.rows, p.N, p.K, ws,
+                               d.gemm, s);
+    float* R = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + d.gemm);
+    for (int h = 0; h < d.halves; ++h) {
+        const char* W = reinterpret_cast<const char*>(p.W) + (int64_t)h * p.N * p.ldw * (w_type == SPLITEE_F32 ? 4 : 2);
+        const int rc = launch_gemm_f32(A, p.lda, W, w_type, p.ldw, nullptr, 0, R + h * (d.ld / 2), d.ld, p.rows, d.n, p.K, ws, d.gemm, s);
+        if (rc != SPLITEE_OK) return rc;
+    }
+    return launch_sum(p, R, 1, s);
+}
+
+}  // namespace
+
 size_t linear_workspace_bytes(int64_t M, int64_t N, int64_t K, int prec, int gated)
 {
-    if (prec == SPLITEE_PREC_F32) return 0;
+    if (prec == SPLITEE_PREC_F32) return f32_dense(M, N, K, gated).bytes;
     const LinPlan plan = plan_linear(M, 1, true, N, K, prec == SPLITEE_PREC_BF16X3 ? 3 : 1, gated);
     return plan.ksplit > 1 ? (size_t)plan.ksplit * M * part_ld(N, gated) * 4 : 0;
 }
 
 int launch_linear(const LinArgs& p, int prec, int w_type, void* ws, hipStream_t s)
 {
-    if (prec == SPLITEE_PREC_F32) {
-        // row tiles of all groups: at most one partly filled one each
-        const int64_t tiles = p.offsets ? p.rows / LS_T + (int64_t)p.experts : (p.rows + LS_T - 1) / LS_T;
-        if (tiles > 65535) return SPLITEE_ERR_UNSUPPORTED;
-        hipLaunchKernelGGL(linear_simple_kernel, dim3((unsigned)((p.N + LS_T - 1) / LS_T), (unsigned)tiles),
-                           dim3(LS_T * LS_T), 0, s, p, prec, w_type);
-        return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
-    }
+    if (prec == SPLITEE_PREC_F32)
+        return p.offsets ? launch_grouped_f32(p, w_type == SPLITEE_BF16, s) : launch_dense_f32(p, w_type, ws, s);
     const bool x3 = prec == SPLITEE_PREC_BF16X3, tiled = w_type == SPLITEE_BF16_TILED;
     const LinPlan plan = plan_linear(p.rows, p.experts, !p.offsets, p.N, p.K, x3 ? 3 : 1, p.gated);
     if (plan.kind == LinPlan::ROWS)
         return x3 ? launch_linear_rows_bf16x3(p, tiled, plan, s) : launch_linear_rows_bf16(p, tiled, plan, s);
     float* part = plan.ksplit > 1 ? reinterpret_cast<float*>(ws) : nullptr;
     const int rc = x3 ? launch_linear_tile_bf16x3(p, tiled, plan, part, s) : launch_linear_tile_bf16(p, tiled, plan, part, s);
-    if (rc != SPLITEE_OK || !part) return rc;
-    const int64_t quads = (int64_t)p.rows * ((p.N + 3) / 4);
-    const int ld = (int)part_ld(p.N, p.gated);
-    if ((quads + 255) / 256 > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((quads + 255) / 256));
-    if (p.gated) hipLaunchKernelGGL(linear_sum_kernel<true>, grid, dim3(256), 0, s, p, part, plan.ksplit, ld);
-    else hipLaunchKernelGGL(linear_sum_kernel<false>, grid, dim3(256), 0, s, p, part, plan.ksplit, ld);
-    return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
+    return rc != SPLITEE_OK || !part ? rc : launch_sum(p, part, plan.ksplit, s);
 }
 
 }  // namespace splitee_host

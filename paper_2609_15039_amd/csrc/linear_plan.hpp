@@ -19,6 +19,8 @@ int launch_linear_rows_bf16x3(const splitee::LinArgs& p, bool tiled, const LinPl
 int launch_linear_tile_bf16(const splitee::LinArgs& p, bool tiled, const LinPlan& plan, float* part, hipStream_t s);
 int launch_linear_tile_bf16x3(const splitee::LinArgs& p, bool tiled, const LinPlan& plan, float* part, hipStream_t s);
 
+int launch_grouped_f32(const splitee::LinArgs& p, bool w_bf16, hipStream_t s);
+
 // Leading dimension of a split's partial product (16-byte rows; of a gated one, gate columns then up columns).
 inline int64_t part_ld(int64_t N, int gated) { return (N + 3) / 4 * 4 * (gated ? 2 : 1); }
 

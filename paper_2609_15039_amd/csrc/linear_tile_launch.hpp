@@ -12,7 +12,7 @@ int tile_run(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, h
     const int64_t nt = (p.N + T::BNO - 1) / T::BNO;
     const int64_t strips = p.offsets ? p.rows / BM + (int64_t)p.experts : (p.rows + BM - 1) / BM;
     const int64_t tiles = strips * nt, nbig = HALF && plan.halve ? tiles / 256 * 256 : tiles;
-    const int64_t wgs = p.offsets ? (tiles + 127) / 128 * 128 // (by expert: the 8 x 16 order)
+    const int64_t wgs = p.offsets ? (tiles + 255) / 256 * 256 // (by expert: the 8 x 32 order)
                                   : (nbig + 2 * (tiles - nbig)) * plan.ksplit;
     if (wgs > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
     const LtPlan lt{(int)nt, plan.ksplit, plan.ktps, part, (int)splitee_host::part_ld(p.N, GATED), (int)nbig};
@@ -36,7 +36,7 @@ int tile_size(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, 
     if (plan.kind == LinPlan::TILE64) return tile_gated<NPL, 64, 128, 2, 2, S, false, TILED>(p, plan, part, s);
     if constexpr (NPL == 1)
         if (plan.kind == LinPlan::TILE256) return tile_gated<1, 256, 256, 2, 4, 2, true, TILED>(p, plan, part, s);
-    if (NPL == 3 && plan.ksplit == 1) return tile_gated<NPL, 128, 256, 2, 4, S, NPL == 3, TILED>(p, plan, part, s);
+    if (plan.ksplit == 1) return tile_gated<NPL, 128, 256, 2, 4, S, true, TILED>(p, plan, part, s);
     return tile_gated<NPL, 128, 256, 2, 4, S, false, TILED>(p, plan, part, s);
 }
 
