@@ -645,26 +645,42 @@ def _expect(ok, what):
         raise ValueError(what)
 
 
-def _here(**tensors):
-    """Every tensor on the current device, whose stream the call takes."""
+def _here(*tensors):
+    """The current device, whose stream the call takes: every tensor is on it."""
     dev = torch.cuda.current_device()
-    for name, t in tensors.items():
-        if t is not None and t.device.index != dev:
-            raise ValueError("%s is on %s, not on the current device" % (name, t.device))
+    for t in tensors:
+        if t is not None and t.get_device() != dev:
+            raise ValueError("a tensor on device %d, the current device is %d" % (t.get_device(), dev))
+    return dev
 
 
 def _matrix(name, t, shape, dtype):
-    _expect(tuple(t.shape) == shape and t.dtype == dtype, "%s: expected %s of %s" % (name, dtype, shape))
-    _expect(t.stride(-1) == 1 or shape[-1] <= 1, "%s: columns are not contiguous" % name)
-    per = 16 // t.element_size()
-    return t.stride(0) if shape[0] > 1 else -(-shape[1] // per) * per  # of a single row no pitch is used
+    """Leading dimension of a matrix of this shape and type."""
+    s0, s1 = t.stride() if t.dim() == 2 else (0, 0)
+    if t.shape != shape or t.dtype != dtype or (s1 != 1 and shape[1] > 1):
+        raise ValueError("%s: expected %s of %s, columns contiguous" % (name, dtype, tuple(shape)))
+    if shape[0] > 1:
+        return s0
+    per = 16 // dtype.itemsize
+    return -(-shape[1] // per) * per  # of a single row no pitch is used
 
 
 def _rows_out(rows, N, dtype, device):
-    """rows x N whose rows begin at multiples of 16 bytes."""
+    """(rows x N whose rows begin at multiples of 16 bytes, leading dimension)"""
     per = 16 // dtype.itemsize
     ld = -(-N // per) * per
-    return torch.empty((rows, ld), dtype=dtype, device=device)[:, :N]
+    out = torch.empty((rows, ld), dtype=dtype, device=device)
+    return (out if ld == N else out[:, :N]), ld
+
+
+def _scratch(nbytes, device):
+    """(address, tensor that holds it) of a 256-byte aligned workspace whose contents do not matter."""
+    if not nbytes:
+        return None, None
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    if buf.data_ptr() % 256:
+        buf = _aligned_bytes(nbytes, device)
+    return buf.data_ptr(), buf
 
 
 def _operand(A, prec):
@@ -686,12 +702,12 @@ def _epilogue(rows, N, NW, C, bias, act, gated, residual, out_dtype, bias_stride
     ep = Epilogue(act=ACTS[act] if isinstance(act, str) else act, gated=1 if gated else 0, out_type=_OUT[out_dtype])
     if C is not None:
         ep.ldc = _matrix("C", C, (rows, NW), torch.float32)
-        ep.C = _ptr(C)
+        ep.C = C.data_ptr()
     if bias is not None:
-        ep.bias, ep.bias_stride = _ptr(bias), bias_stride
+        ep.bias, ep.bias_stride = bias.data_ptr(), bias_stride
     if residual is not None:
         ep.ldres = _matrix("residual", residual, (rows, N), out_dtype)
-        ep.residual = _ptr(residual)
+        ep.residual = residual.data_ptr()
     return ep
 
 
@@ -709,18 +725,24 @@ def linear_epilogue(A, prec, W, C=None, bias=None, act="none", gated=False, resi
     _expect(len(W.shape) == 2 and W.shape[1] == K, "W: expected N x %d" % K)
     _expect(W.stride(1) == 1 or K <= 1, "W: columns are not contiguous")
     N = _out_width(NW, gated)
-    _here(A=A, W=W, C=C, bias=bias, residual=residual, Y=Y)
+    dev = _here(A, W.data if isinstance(W, TiledWeights) else W, C, bias, residual, Y)
     if bias is not None:
         _expect(tuple(bias.shape) == (NW,) and bias.dtype == torch.float32 and (NW < 2 or bias.stride(0) == 1),
                 "bias: expected %d contiguous float32" % NW)
     ep = _epilogue(M, N, NW, C, bias, act, gated, residual, out_dtype)
     if Y is None:
-        Y = _rows_out(M, N, out_dtype, A.device)
-    ldy = _matrix("Y", Y, (M, N), out_dtype)
+        Y, ldy = _rows_out(M, N, out_dtype, A.device)
+    else:
+        ldy = _matrix("Y", Y, (M, N), out_dtype)
+    lib = load()
     if ws is None:
-        nbytes = splitee_epilogue_workspace_bytes(M, N, K, prec, gated)
-        ws = (_aligned_bytes(nbytes, A.device) if nbytes else None, nbytes)
-    splitee_linear_epilogue(A, prec, lda, W, _wtype(W), W.stride(0) if NW > 1 and K else K, ep, Y, ldy, M, N, K, ws[0], ws[1])
+        nbytes = lib.splitee_epilogue_workspace_bytes(M, N, K, prec, ep.gated)
+        ws, held = _scratch(nbytes, A.device)
+    else:
+        ws, nbytes = _ptr(ws[0]), ws[1]
+    _check("splitee_linear_epilogue", lib.splitee_linear_epilogue(
+        A.data_ptr(), prec, lda, W.data_ptr(), _wtype(W), W.stride(0) if NW > 1 and K else K, ctypes.byref(ep), Y.data_ptr(), ldy,
+        M, N, K, ws, nbytes, torch._C._cuda_getCurrentRawStream(dev)))
     return Y
 
 
@@ -735,7 +757,7 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
     experts = (W.data if tiled else W).shape[0]
     NW = W.shape[-2]
     N = _out_width(NW, gated)
-    _here(A=A, W=W, offsets=offsets, row_index=row_index, C=C, bias=bias, residual=residual, Y=Y)
+    dev = _here(A, W.data if tiled else W, offsets, row_index, C, bias, residual, Y)
     for name, t, n in (("offsets", offsets, experts + 1), ("row_index", row_index, None)):
         _expect(t is None or t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and n in (None, t.numel()),
                 "%s: expected contiguous int32%s" % (name, " of experts + 1" if n else ""))
@@ -752,10 +774,13 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
                 "bias: expected float32 of experts x %d" % NW)
     ep = _epilogue(rows, N, NW, C, bias, act, gated, residual, out_dtype, 0 if bias is None else bias.stride(0))
     if Y is None:
-        Y = _rows_out(rows, N, out_dtype, A.device)
-    ldy = _matrix("Y", Y, (rows, N), out_dtype)
-    splitee_grouped_linear(A, prec, lda, a_rows, row_index, offsets, experts, W, _wtype(W), ldw, w_stride, ep, Y, ldy,
-                           rows, N, K)
+        Y, ldy = _rows_out(rows, N, out_dtype, A.device)
+    else:
+        ldy = _matrix("Y", Y, (rows, N), out_dtype)
+    _check("splitee_grouped_linear", load().splitee_grouped_linear(
+        A.data_ptr(), prec, lda, a_rows, None if row_index is None else row_index.data_ptr(), offsets.data_ptr(), experts,
+        W.data_ptr(), _wtype(W), ldw, w_stride, ctypes.byref(ep), Y.data_ptr(), ldy, rows, N, K,
+        torch._C._cuda_getCurrentRawStream(dev)))
     return Y
 
 
@@ -782,16 +807,21 @@ def route(logits, k, score="softmax", renorm=True, ws=None):
     _expect(logits.dim() == 2 and logits.dtype == torch.float32, "logits: expected float32 of tokens x experts")
     T, E = logits.shape
     _expect(logits.stride(1) == 1 or E <= 1, "logits: columns are not contiguous")
-    _here(logits=logits)
+    here = _here(logits)
     dev, i32 = logits.device, torch.int32
     r = Routes(torch.empty((T, k), dtype=i32, device=dev), torch.empty((T, k), dtype=torch.float32, device=dev),
                torch.empty(E + 1, dtype=i32, device=dev), torch.empty(T * k, dtype=i32, device=dev),
                torch.empty((T, k), dtype=i32, device=dev))
+    lib = load()
     if ws is None:
-        nbytes = splitee_route_workspace_bytes(T, E, k)
-        ws = (_aligned_bytes(nbytes, dev), nbytes)
-    splitee_route(logits, logits.stride(0) if T > 1 else E, T, E, k, SCORES[score] if isinstance(score, str) else score,
-                  renorm, r.experts, r.weights, r.offsets, r.row_index, r.slot, ws[0], ws[1])
+        nbytes = lib.splitee_route_workspace_bytes(T, E, k)
+        ws, held = _scratch(nbytes, dev)
+    else:
+        ws, nbytes = _ptr(ws[0]), ws[1]
+    _check("splitee_route", lib.splitee_route(
+        logits.data_ptr(), logits.stride(0) if T > 1 else E, T, E, k, SCORES[score] if isinstance(score, str) else score,
+        1 if renorm else 0, r.experts.data_ptr(), r.weights.data_ptr(), r.offsets.data_ptr(), r.row_index.data_ptr(),
+        r.slot.data_ptr(), ws, nbytes, torch._C._cuda_getCurrentRawStream(here)))
     return r
 
 
@@ -802,11 +832,15 @@ def combine(H, slot, weights, residual=None, out_dtype=torch.float32, Y=None):
             and weights.dtype == torch.float32 and weights.is_contiguous(),
             "slot, weights: expected contiguous int32 and float32 of tokens x k")
     (h_rows, N), (T, k) = H.shape, slot.shape
-    _here(H=H, slot=slot, weights=weights, residual=residual, Y=Y)
+    dev = _here(H, slot, weights, residual, Y)
     ldh = _matrix("H", H, (h_rows, N), H.dtype)
     ldres = _matrix("residual", residual, (T, N), out_dtype) if residual is not None else 0
     if Y is None:
-        Y = _rows_out(T, N, out_dtype, H.device)
-    splitee_combine(H, _OUT[H.dtype], ldh, h_rows, slot, weights, residual, ldres, Y, _OUT[out_dtype],
-                    _matrix("Y", Y, (T, N), out_dtype), T, k, N)
+        Y, ldy = _rows_out(T, N, out_dtype, H.device)
+    else:
+        ldy = _matrix("Y", Y, (T, N), out_dtype)
+    _check("splitee_combine", load().splitee_combine(
+        H.data_ptr(), _OUT[H.dtype], ldh, h_rows, slot.data_ptr(), weights.data_ptr(),
+        None if residual is None else residual.data_ptr(), ldres, Y.data_ptr(), _OUT[out_dtype], ldy, T, k, N,
+        torch._C._cuda_getCurrentRawStream(dev)))
     return Y
