@@ -42,52 +42,61 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinArgs p, const float*
 
 namespace splitee_host {
 
-// The cheapest kernel by a model of the launch's time in microseconds, fitted to products of 1-4096 rows (1-64
-// experts), 2560-9728 wide W dense and 768 x 2048 by expert:
-//  few rows   5 + the larger of 5.5e-4 a workgroup and K tile (the rate of W from HBM) and 0.5 a K tile of a wave;
-//  64 x 128   6 + rounds of 512 workgroups (two a CU) times K tiles at 0.70 us (three planes 1.06), 0.30 (0.90)
-//             where each CU has one workgroup at most;
-//  128 x 256  8 + rounds of 256 workgroups times K tiles at 1.0 us (2.15);
-//  a split K  4 + its partial products written and read at 4 TB/s.
-// groups: experts (1: dense, whose K may be split).  By expert only the total of the rows is known here: as many groups as
-// there can be have rows, and each ends with half a tile.
+// The cheapest kernel by a model of the launch's time in microseconds, fitted to products of 1-4000 rows with 256-9728
+// wide W dense, and of 8-48000 rows of 8-64 experts, W not in any cache (within 15% of most of them):
+//  few rows   5 + the largest of W at 5.3 TB/s (16 rows of three planes: 4.4), 6.2e-4 (6.5e-4) a workgroup and K tile, and
+//             0.5 a K tile of a wave;
+//  64 x 128   6 + the larger of W at 4.8 TB/s and rounds of 512 workgroups (two a CU) times K tiles at 0.30 us (three
+//             planes 0.90) where each CU has one at most, 0.85 (1.40) where it has two;
+//  128 x 256  8 + rounds of 256 times K tiles at 1.0 us (2.2), 0.65 (1.8) where a quarter of the CUs is idle;
+//  256 x 256  12 + rounds of 256 times K tiles at 1.5 us;
+//  a split K  2 + its partial products written and read at 6 TB/s.
+// Both sides of the borders, us: 512 rows of 64 experts (768 gated x 2048), few rows 80 and 64 x 128 88, 1024 rows 100 and
+// 95; 100 rows of gate/up in three planes, 64 x 128 in three splits 54 and 128 x 256 in three 46; 333 rows of down, 33
+// either way; 48000 rows of 64 experts 128 x 256 352, 256 x 256 357; 4096 rows x 9728 x 2560, 128 x 256 228, 256 x 256 207.
+// groups: experts.  By expert only the total of the rows is known here: experts are taken to be chosen evenly, and each
+// ends with half a tile.
 LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t K, int npl, int gated)
 {
-    const int64_t kt = std::max<int64_t>(1, (K + 63) / 64), live = std::max<int64_t>(1, std::min(groups, rows));
-    auto strips = [&](int bm) {
-        return dense ? (double)((rows + bm - 1) / bm) : live * std::max(1.0, (double)rows / live / bm + 0.5);
-    };
+    const int64_t kt = std::max<int64_t>(1, (K + 63) / 64);
+    const double live = dense ? 1.0 : std::max(1.0, groups * (1.0 - std::exp(-(double)rows / groups)));
+    const double wbytes = live * N * (gated ? 2 : 1) * K * 2.0;
+    auto strips = [&](int bm) { return dense ? (double)((rows + bm - 1) / bm) : live * std::max(1.0, rows / live / bm + 0.5); };
+    const bool x3 = npl == 3;
     LinPlan best{};
     best.cost = 1e30;
     for (int bm = 8; bm <= 16; bm *= 2) {
         LinPlan p{LinPlan::ROWS, bm, 2, 4, 1, (int)kt, false, 0.0};
         auto wgs = [&]() { const int bno = 16 * p.tn / (gated ? 2 : 1); return strips(bm) * ((N + bno - 1) / bno); };
-        if (!gated && wgs() < 256) p.tn = 1; // 16 columns each: more CUs at work
+        if (!gated && wgs() < 128) p.tn = 1; // 16 columns each: more CUs at work
         // eight waves where K is long and their stages leave room for two workgroups, or there are few
         if (kt >= 32 && (npl * bm <= 24 || wgs() <= 256)) p.nw = 8;
-        p.cost = 5 + std::max(wgs() * kt * 5.5e-4 * p.tn / 2, (double)((kt + p.nw - 1) / p.nw) * 0.5);
+        p.cost = 5 + std::max({wbytes / (x3 && bm == 16 ? 4.4e6 : 5.3e6), wgs() * kt * (x3 ? 6.5e-4 : 6.2e-4) * p.tn / 2,
+                               (double)((kt + p.nw - 1) / p.nw) * 0.5});
         if (p.cost < best.cost) best = p;
     }
-    // microseconds of a K tile, alone on a CU (64 x 128) or with as many as fit, and of all else
-    struct Tile { LinPlan::Kind kind; int bm, bn, slots; double alone, full, fixed; bool split, halves; };
+    // microseconds of a K tile, with few and with many workgroups, and of all else
+    struct Tile { LinPlan::Kind kind; int bm, bn, slots; double few, full, fixed; bool split, halves; };
     const Tile tiles[] = {
-        {LinPlan::TILE64, 64, 128, 512, npl == 1 ? 0.30 : 0.90, npl == 1 ? 0.80 : 1.40, 6, true, false},
-        {LinPlan::TILE128, 128, 256, 256, npl == 1 ? 1.0 : 2.15, npl == 1 ? 1.0 : 2.15, 8, true, true},
+        {LinPlan::TILE64, 64, 128, 512, x3 ? 0.90 : 0.30, x3 ? 1.40 : 0.85, 6, true, false},
+        {LinPlan::TILE128, 128, 256, 256, x3 ? 1.8 : 0.65, x3 ? 2.2 : 1.0, 8, true, true},
         {LinPlan::TILE256, 256, 256, 256, 1.5, 1.5, 12, false, true}};
     for (const Tile& t : tiles) {
-        if (t.kind == LinPlan::TILE256 && (npl != 1 || !dense)) continue;
+        if (t.kind == LinPlan::TILE256 && (x3 || !dense)) continue;
         const int bno = t.bn / (gated ? 2 : 1);
         const double n = strips(t.bm) * ((N + bno - 1) / bno);
         const int most = dense && t.split ? (int)std::min<int64_t>(8, std::max<int64_t>(1, kt / 4)) : 1;
         for (int ks = 1; ks <= most; ++ks) {
             LinPlan p{t.kind, 0, 0, 0, ks, (int)((kt + ks - 1) / ks), false, 0.0};
             if ((int64_t)(ks - 1) * p.ktps >= kt) continue; // a split without K tiles
-            const double wgs = n * ks, rounds = std::floor(wgs / t.slots);
-            const double round = p.ktps * (t.alone + (t.full - t.alone) * std::min(1.0, std::max(0.0, (wgs - 256) / 256)));
-            const double rest = wgs - rounds * t.slots;
-            p.halve = dense && t.halves && ks == 1 && rest > 0 && rest <= t.slots / 2;
-            p.cost = t.fixed + rounds * round + (rest == 0 ? 0 : p.halve ? 0.62 * round : !dense && rounds >= 2 ? rest / t.slots * round : round);
-            if (ks > 1) p.cost += 4 + ks * rows * part_ld(N, gated) * 8.0 / 4e6;
+            const double wgs = n * ks, rounds = std::floor(wgs / t.slots), rest = wgs - rounds * t.slots;
+            const double fill = (rest - (t.kind == LinPlan::TILE64 ? 256 : 192)) / 64; // of the last round
+            const double last = rest == 0 ? 0.0 : p.ktps * (t.few + (t.full - t.few) * std::min(1.0, std::max(0.0, fill)));
+            p.halve = dense && t.halves && ks == 1 && rest > 0 && rest <= t.slots / 2 && rounds > 0;
+            const double time = rounds * p.ktps * t.full + (p.halve ? 0.62 * p.ktps * t.full
+                                                            : !dense && rounds >= 2 ? rest / t.slots * p.ktps * t.full : last);
+            p.cost = t.fixed + std::max(time, wbytes / 4.8e6);
+            if (ks > 1) p.cost += 2 + ks * rows * part_ld(N, gated) * 8.0 / 6e6;
             if (p.cost < best.cost) best = p;
         }
     }
