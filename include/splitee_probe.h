@@ -74,6 +74,14 @@ int splitee_spectral_norm_probe(const void* W, int w_type, int64_t ldw, int64_t 
                                 uint64_t seed, uint64_t stream_id, double* sigma, double* history,
                                 void* workspace, size_t workspace_bytes, int64_t spins, int* path, void* stream);
 
+/*
+ * Which kernel splitee_linear_epilogue (dense != 0) or splitee_grouped_linear (groups experts) takes for this
+ * shape in BF16 or BF16X3; host only, SPLITEE_ERR_ARG on arguments that those calls refuse or that have no plan (F32).
+ *   plan   receives kind (0 few rows, 1 64 x 128 tiles, 2 128 x 256, 3 256 x 256), rows, 16-row weight blocks and
+ *          waves of a few-row workgroup (0 for tiles), splits of K, and 1 if the last round's tiles are halved
+ */
+int splitee_linear_plan_probe(int64_t rows, int64_t groups, int dense, int64_t N, int64_t K, int prec, int gated, int* plan);
+
 #ifdef __cplusplus
 }
 #endif

@@ -38,7 +38,8 @@ EXPORTED = [
     "splitee_route_workspace_bytes", "splitee_route", "splitee_combine",
 ]
 # test hooks (include/splitee_probe.h)
-EXPORTED_PROBE = ["splitee_transform_probe", "splitee_mfma_probe", "splitee_spectral_norm_probe"]
+EXPORTED_PROBE = ["splitee_transform_probe", "splitee_mfma_probe", "splitee_spectral_norm_probe",
+                  "splitee_linear_plan_probe"]
 SPLITEE_PATH_NONE, SPLITEE_PATH_STREAMED, SPLITEE_PATH_RESIDENT, SPLITEE_PATH_GAVE_UP = 0, 1, 2, 3
 SPLITEE_PREC_F64 = 3
 SPLITEE_ERR_IO, SPLITEE_ERR_EXHAUSTED, SPLITEE_ERR_FORMAT, SPLITEE_ERR_BUSY = -8, -9, -10, -11
@@ -130,6 +131,7 @@ def load():
         "splitee_spectral_norm_probe": (I, [P, I, I64, I64, I64, I, U64, U64, P, P, P, SZ, I64, P, P]),
         "splitee_masked_linear_fused_noalloc": (I, [P, I64, P, I, I64, P, I64, P, I64, I64, I64, I64, I, D, D,
                                                     U64, U64, U64, P, I, P]),
+        "splitee_linear_plan_probe": (I, [I64, I64, I, I64, I64, I, I, P]),
         "splitee_epilogue_workspace_bytes": (SZ, [I64, I64, I64, I, I]),
         "splitee_linear_epilogue": (I, [P, I, I64, P, I, I64, P, P, I64, I64, I64, I64, P, SZ, P]),
         "splitee_grouped_linear": (I, [P, I, I64, I64, P, P, I64, P, I, I64, I64, P, P, I64, I64, I64, I64, P]),
@@ -458,6 +460,14 @@ def splitee_grouped_linear(A, in_prec, lda, a_rows, row_index, offsets, experts,
     _check("splitee_grouped_linear", load().splitee_grouped_linear(
         _ptr(A), in_prec, lda, a_rows, _ptr(row_index), _ptr(offsets), experts, _ptr(W), w_type, ldw, w_stride,
         ctypes.byref(ep), _ptr(Y), ldy, rows, N, K, _stream(stream)))
+
+
+def splitee_linear_plan_probe(rows, groups, dense, N, K, prec, gated):
+    """(kind, rows, weight blocks, waves, splits, halved); see splitee_probe.h."""
+    plan = (ctypes.c_int * 6)()
+    _check("splitee_linear_plan_probe", load().splitee_linear_plan_probe(
+        rows, groups, 1 if dense else 0, N, K, prec, 1 if gated else 0, ctypes.cast(plan, ctypes.c_void_p)))
+    return tuple(plan)
 
 
 def splitee_route_workspace_bytes(T, E, k):
@@ -844,3 +854,44 @@ def combine(H, slot, weights, residual=None, out_dtype=torch.float32, Y=None):
         None if residual is None else residual.data_ptr(), ldres, Y.data_ptr(), _OUT[out_dtype], ldy, T, k, N,
         torch._C._cuda_getCurrentRawStream(dev)))
     return Y
+
+
+def _mask_planes(X, rows, K, prec, mech, sensitivity, epsilon, seed, stream_id, row0, device):
+    """noise_mask of X, or (X None) of zeros: the planes of the mask itself."""
+    planes = 3 if prec == SPLITEE_PREC_BF16X3 else 1
+    Xt = torch.empty((planes, rows, K), dtype=torch.float32 if prec == SPLITEE_PREC_F32 else torch.int16, device=device)
+    splitee_noise_mask(X, K if X is None else X.stride(0), Xt, prec, K, rows, K, mech, sensitivity, epsilon, seed, stream_id, row0)
+    return Xt
+
+
+def expert_ffn(X, logits, k, W_gate_up, W_down, mech=SPLITEE_MECH_NONE, sensitivity=0.0, epsilon=1.0, seed=0, stream_id=0,
+               row0=0, prec=SPLITEE_PREC_BF16X3, act="silu", score="softmax", renorm=True, residual=None,
+               out_dtype=torch.float32):
+    """The feed-forward part of a mixture-of-experts layer under masks: route the tokens, mask them, the experts' gate
+    and up projections unmasked and gated, mask the result, the experts' down projections unmasked, and the
+    weighted sum, plus the residual.
+
+    X: tokens x K float32; logits: tokens x experts float32; W_gate_up: experts x 2 N x K and W_down: experts x D x N,
+    bfloat16 tensors or the TiledWeights of tile_experts (float32 with SPLITEE_PREC_F32), K and N multiples of 8.  The
+    masks are rows row0 .. of noise stream stream_id (gate and up: a token has one mask for all its experts) and rows
+    row0 k .. of stream stream_id + 1 (down: one for each row in the router's order).  As in the fused call the
+    corrections are formed on this GPU, here once the rows' experts are known; SPLITEE_MECH_NONE is the split without
+    noise, which has none."""
+    T, K = X.shape
+    N = W_down.shape[-1]
+    r = route(logits, k, score=score, renorm=renorm)
+    noise_args = (mech, sensitivity, epsilon, seed)
+    masked = mech != SPLITEE_MECH_NONE
+    exact = SPLITEE_PREC_F32 if prec == SPLITEE_PREC_F32 else SPLITEE_PREC_BF16X3  # of a correction
+
+    def projection(A, rows, width, W, sid, first, index, **epilogue):
+        C = None
+        if masked:
+            eta = _mask_planes(None, rows, width, exact, *noise_args, sid, first, X.device)
+            C = grouped_linear(eta, exact, W, r.offsets, row_index=index)
+        At = _mask_planes(A, rows, width, prec, *noise_args, sid, first, X.device)
+        return grouped_linear(At, prec, W, r.offsets, row_index=index, C=C, **epilogue)
+
+    H = projection(X, T, K, W_gate_up, stream_id, row0, r.row_index, act=act, gated=True)
+    R = projection(H, T * k, N, W_down, stream_id + 1, row0 * k, None)
+    return combine(R, r.slot, r.weights, residual=residual, out_dtype=out_dtype)

@@ -1,7 +1,8 @@
 // C ABI of the projections with an epilogue and of the expert path: argument validation and kernel
 // launches.  Semantics of every entry point are documented in include/splitee.h.
 #include "api_checks.hpp"
-#include "epilogue_dev.hpp"
+#include "linear_plan.hpp"
+#include "splitee_probe.h"
 
 namespace splitee_host {
 // Bytes of the partial tiles of a dense product whose K is split (0: not split).
@@ -122,6 +123,22 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
     p.experts = (int)experts;
     p.w_stride = w_stride;
     return splitee_host::launch_linear(p, in_prec, w_type, nullptr, as_stream(stream));
+}
+
+int splitee_linear_plan_probe(int64_t rows, int64_t groups, int dense, int64_t N, int64_t K, int prec, int gated, int* plan)
+{
+    if (!plan || (prec != SPLITEE_PREC_BF16 && prec != SPLITEE_PREC_BF16X3) || !dims_ok(rows, N, K) || rows < 1 || N < 1 ||
+        groups < 1 || groups > MAX_DIM || K % 8 != 0 || gated < 0 || gated > 1)
+        return SPLITEE_ERR_ARG;
+    const splitee_host::LinPlan p = splitee_host::plan_linear(rows, groups, dense != 0, N, K, prec == SPLITEE_PREC_BF16X3 ? 3 : 1, gated);
+    const bool few = p.kind == splitee_host::LinPlan::ROWS;
+    plan[0] = (int)p.kind;
+    plan[1] = few ? p.bm : 0;
+    plan[2] = few ? p.tn : 0;
+    plan[3] = few ? p.nw : 0;
+    plan[4] = p.ksplit;
+    plan[5] = p.halve ? 1 : 0;
+    return SPLITEE_OK;
 }
 
 size_t splitee_route_workspace_bytes(int64_t T, int64_t E, int64_t k)

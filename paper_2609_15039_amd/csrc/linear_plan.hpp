@@ -13,6 +13,8 @@ struct LinPlan {
     double cost;    // microseconds
 };
 
+LinPlan plan_linear(int64_t rows, int64_t groups, bool dense, int64_t N, int64_t K, int npl, int gated);
+
 // launches of one kernel family; part: the partial tiles of a split K, or null
 int launch_linear_rows_bf16(const splitee::LinArgs& p, bool tiled, const LinPlan& plan, hipStream_t s);
 int launch_linear_rows_bf16x3(const splitee::LinArgs& p, bool tiled, const LinPlan& plan, hipStream_t s);
