@@ -45,7 +45,7 @@ struct LtPlan {
     int ksplit, ktps;    // splits of K and K tiles of one
     float* part;         // partial tiles of a split K: split s at part + s * rows * ldpart, row-major; of a gated product
     int ldpart;          // gate columns, then from ldpart / 2 up columns
-    int nbig;            // HALF, dense: tiles that are not halved
+    int nhalf;           // HALF, dense: workgroups with half tiles, of which two make one of the first nhalf / 2 tiles
 };
 
 template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED>
@@ -303,8 +303,9 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
     }
 }
 
-// HALF: the tiles from plan.nbig on are computed as two of BM / 2 rows, and so is a tile with at most BM / 2 rows:
-// the last, partly filled round of workgroups then takes little more than half a round's time.
+// HALF: plan.nhalf workgroups take half tiles of BM / 2 rows, and so is a tile with at most BM / 2 rows computed: a partly
+// filled round of workgroups then takes little more than half a round's time.  They come first, so that the CUs end
+// their tiles, and write them, at different times.
 template <int NPL, int BM, int BN, int WGM, int WGN, int S, bool GATED, bool TILED, bool HALF>
 __global__ void __launch_bounds__(WGM * WGN * WAVE)
 lin_tile_kernel(const LinArgs p, const LtPlan plan)
@@ -317,12 +318,13 @@ lin_tile_kernel(const LinArgs p, const LtPlan plan)
         constexpr int C = 32;
         const int b = blockIdx.x, x = b % 8, i = b / 8;
         L = (i / C) * (8 * C) + x * C + i % C;
-    } else if (HALF && (int)blockIdx.x >= plan.nbig) {
-        const int h = (int)splitee::xcd_logical_block(blockIdx.x - plan.nbig, gridDim.x - plan.nbig);
-        L = plan.nbig + h / 2;
+    } else if (HALF && (int)blockIdx.x < plan.nhalf) {
+        const int h = (int)splitee::xcd_logical_block(blockIdx.x, (uint32_t)plan.nhalf);
+        L = h / 2;
         half = 1 + h % 2;
     } else {
-        L = (int)splitee::xcd_logical_block(blockIdx.x, HALF ? (uint32_t)plan.nbig : gridDim.x);
+        const uint32_t first = HALF ? (uint32_t)plan.nhalf : 0u;
+        L = (int)splitee::xcd_logical_block(blockIdx.x - first, gridDim.x - first) + (int)first / 2;
         split = L % plan.ksplit;
         L /= plan.ksplit;
     }
