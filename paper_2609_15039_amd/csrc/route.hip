@@ -1,12 +1,13 @@
 // Router of a mixture-of-experts layer and the weighted sum that ends it (gfx950): splitee_route and
 // splitee_combine.
 //
-// Router.  A wave takes a token: its E logits lie in the lanes' registers (expert i in lane i % 64, register
-// i / 64) as integers in the logits' order, and the k choices are k rounds of a wave-wide maximum by DPP (six
-// instructions and a lane read; by shuffles through LDS the 8000 x 256 case took 71 us here), the lowest index among
-// equals found by ballots, register by register.  The next token's logits are on their way meanwhile.  The rows of an
+// Router.  A wave takes two tokens: the E logits of each lie in the lanes' registers as integers in the logits' order,
+// consecutive experts in a lane, which sorts its own once.  The k choices are k rounds of a maximum of the lanes' heads by
+// DPP (six instructions and a lane read), the lowest lane among equals found by a ballot, and a shift in that lane: about
+// 20 vector instructions a choice, which is what bounds it.  (8000 x 256: 71 us with the maxima by shuffles through
+// LDS, 11 us without the sorting, where each choice looked through all registers.)  The rows of an
 // expert are numbered by token without atomics whose order could show: a workgroup keeps for every expert a bit mask
-// of its 64 tokens, so that a choice's place among the workgroup's rows is a population count, and the workgroups'
+// of its tokens, so that a choice's place among the workgroup's rows is a population count, and the workgroups'
 // counts are summed in order: for one workgroup in the same launch, up to 32 by each workgroup for itself, above by a
 // launch of their own.
 // Combine.  Bound by memory: each row read once, 16 bytes a lane, all of a token's rows in flight together.
@@ -14,27 +15,32 @@
 
 namespace {
 
-constexpr int RT_TOKENS = 64; // tokens of a workgroup: bits of a mask
+constexpr int RT_ONE = 64;    // most tokens of a launch of one workgroup
+constexpr int RT_TOKENS = 32; // tokens of a workgroup of several: two for each wave, and enough workgroups for the chip
 constexpr int RT_WAVES = 16, RT_NT = RT_WAVES * 64;
 constexpr int RT_MAX_E = 1024;
 constexpr int RT_MAX_K = 64;
 constexpr int RT_FEW = 32; // workgroups whose counts each of them sums itself
 
-// lane 63: the maximum / the sum (in a fixed order) over the wave.  A lane without a source keeps its own value.
+// The maximum / the sum (in a fixed order) over the wave, which lane 63 ends with.
 template <int CTRL, int ROWS>
 __device__ __forceinline__ int dpp(int old, int v)
 {
     return __builtin_amdgcn_update_dpp(old, v, CTRL, ROWS, 0xF, false);
 }
-__device__ __forceinline__ int wave_max(int v)
+__device__ __forceinline__ void wave_max(int& a, int& b)
 {
-    v = max(v, dpp<0x111, 0xF>(v, v)); // row_shr:1, 2, 4, 8: lane 15 of each row of 16
-    v = max(v, dpp<0x112, 0xF>(v, v));
-    v = max(v, dpp<0x114, 0xF>(v, v));
-    v = max(v, dpp<0x118, 0xF>(v, v));
-    v = max(v, dpp<0x142, 0xA>(v, v)); // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
-    v = max(v, dpp<0x143, 0xC>(v, v));
-    return __builtin_amdgcn_readlane(v, 63);
+    // (a lane without a source gets the least integer, which the compiler folds into one v_max_i32_dpp)
+#define RT_STEP(CTRL, ROWS) a = max(a, dpp<CTRL, ROWS>(INT32_MIN, a)); b = max(b, dpp<CTRL, ROWS>(INT32_MIN, b))
+    RT_STEP(0x111, 0xF); // row_shr:1, 2, 4, 8: lane 15 of each row of 16
+    RT_STEP(0x112, 0xF);
+    RT_STEP(0x114, 0xF);
+    RT_STEP(0x118, 0xF);
+    RT_STEP(0x142, 0xA); // row_bcast:15 into rows 1 and 3, row_bcast:31 into rows 2 and 3
+    RT_STEP(0x143, 0xC);
+#undef RT_STEP
+    a = __builtin_amdgcn_readlane(a, 63);
+    b = __builtin_amdgcn_readlane(b, 63);
 }
 template <int CTRL, int ROWS>
 __device__ __forceinline__ float dpp_add(float v)
@@ -89,70 +95,97 @@ route_topk_kernel(const float* __restrict__ logits, int64_t ldl, int T, int E, i
                   int32_t* __restrict__ experts, float* __restrict__ weights, int32_t* __restrict__ slot,
                   int32_t* __restrict__ counts, int32_t* __restrict__ offsets, int32_t* __restrict__ row_index)
 {
-    __shared__ uint32_t mask[2][RT_MAX_E];
-    __shared__ int16_t chosen[RT_TOKENS * RT_MAX_K];
+    constexpr int TOKENS = ONE ? RT_ONE : RT_TOKENS;
+    __shared__ uint32_t mask[TOKENS / 32][RT_MAX_E];
+    __shared__ int16_t chosen[TOKENS * RT_MAX_K];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    const int t0 = blockIdx.x * RT_TOKENS, tokens = min(RT_TOKENS, T - t0);
-    for (int e = tid; e < E; e += RT_NT) mask[0][e] = mask[1][e] = 0u;
-    float x[V];
-    auto fetch = [&](int i) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) x[v] = 64 * v + lane < E ? logits[(int64_t)(t0 + i) * ldl + 64 * v + lane] : -INFINITY;
-    };
-    if (wave < tokens) fetch(wave);
+    const int t0 = blockIdx.x * TOKENS, tokens = min(TOKENS, T - t0);
+    for (int e = tid; e < E; e += RT_NT) mask[0][e] = mask[TOKENS / 32 - 1][e] = 0u;
     __syncthreads();
-    for (int i = wave; i < tokens; i += RT_WAVES) {
-        const int64_t t = t0 + i;
-        int l[V];
+    // two tokens at a time: one's instructions fill the waits of the other's
+    for (int i0 = 2 * wave; i0 < tokens; i0 += 2 * RT_WAVES) {
+        // a lane has experts V lane .. V lane + V - 1, largest first and equal ones by rising index: l[.][0] is its
+        // head, of[.][v] the place of l[.][v] among them
+        int l[2][V], of[2][V], mine[2], best[2];
+        float m[2] = {0.f, 0.f}, total[2] = {0.f, 0.f}, x[2][V];
+        // every load unconditional (past the experts: the last), so that they are in flight together
 #pragma unroll
-        for (int v = 0; v < V; ++v) l[v] = key_of(x[v]);
-        if (i + RT_WAVES < tokens) fetch(i + RT_WAVES);
-        float m = 0.f, total = 0.f;
-        // lane j keeps choice j
-        int mine = -1, best = RT_MASKED;
-        for (int j = 0; j < k; ++j) {
-            int top = l[0];
+        for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int v = 1; v < V; ++v) top = max(top, l[v]);
-            top = wave_max(top);
-            if (top == RT_MASKED) break; // every expert left is masked
-            if (j == 0) {
-                m = of_key(top);
-                if (score == SPLITEE_SCORE_SOFTMAX && !renorm) {
+            for (int v = 0; v < V; ++v)
+                x[q][v] = logits[(int64_t)(t0 + min(i0 + q, tokens - 1)) * ldl + min(V * lane + v, E - 1)];
 #pragma unroll
-                    for (int v = 0; v < V; ++v) total += l[v] == RT_MASKED ? 0.f : expf(of_key(l[v]) - m);
-                    total = wave_sum(total);
-                }
-            }
-            int e = -1;
+        for (int q = 0; q < 2; ++q) {
+            mine[q] = -1; // lane j keeps choice j
+            best[q] = RT_MASKED;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const uint64_t at = __ballot(l[v] == top);
-                if (e < 0 && at) {
-                    const int src = __ffsll((unsigned long long)at) - 1;
-                    e = 64 * v + src;
-                    if (lane == src) l[v] = RT_MASKED;
+                l[q][v] = V * lane + v < E ? key_of(x[q][v]) : RT_MASKED;
+                of[q][v] = v;
+            }
+#pragma unroll
+            for (int n = V - 1; n > 0; --n) // exchanges of neighbours, which leave equal ones in their order
+#pragma unroll
+                for (int v = 0; v < n; ++v) {
+                    const bool swap = l[q][v] < l[q][v + 1];
+                    const int big = max(l[q][v], l[q][v + 1]), low = min(l[q][v], l[q][v + 1]);
+                    const int ob = swap ? of[q][v + 1] : of[q][v], ol = swap ? of[q][v] : of[q][v + 1];
+                    l[q][v] = big; l[q][v + 1] = low;
+                    of[q][v] = ob; of[q][v + 1] = ol;
+                }
+        }
+        for (int j = 0; j < k; ++j) {
+            int top[2] = {l[0][0], l[1][0]};
+            wave_max(top[0], top[1]);
+            if (j == 0) {
+#pragma unroll
+                for (int q = 0; q < 2; ++q) {
+                    m[q] = of_key(top[q]);
+                    if (score == SPLITEE_SCORE_SOFTMAX && !renorm) {
+#pragma unroll
+                        for (int v = 0; v < V; ++v) total[q] += l[q][v] == RT_MASKED ? 0.f : expf(of_key(l[q][v]) - m[q]);
+                        total[q] = wave_sum(total[q]);
+                    }
                 }
             }
-            if (lane == j) {
-                mine = e;
-                best = top;
+            if (top[0] == RT_MASKED && top[1] == RT_MASKED) break; // every expert left is masked
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const int src = __ffsll((unsigned long long)__ballot(l[q][0] == top[q])) - 1; // the lowest of equal ones
+                const int e = V * src + __builtin_amdgcn_readlane(of[q][0], src);
+                const bool taken = lane == src;
+#pragma unroll
+                for (int v = 0; v + 1 < V; ++v) {
+                    l[q][v] = taken ? l[q][v + 1] : l[q][v];
+                    of[q][v] = taken ? of[q][v + 1] : of[q][v];
+                }
+                l[q][V - 1] = taken ? RT_MASKED : l[q][V - 1];
+                if (lane == j && top[q] != RT_MASKED) {
+                    mine[q] = e;
+                    best[q] = top[q];
+                }
             }
         }
-        const float b = of_key(best);
-        float w = mine < 0 ? 0.f : score == SPLITEE_SCORE_SOFTMAX ? expf(b - m) : 1.0f / (1.0f + expf(-b));
-        if (renorm) total = wave_sum(w);
-        if ((renorm || score == SPLITEE_SCORE_SOFTMAX) && total != 0.f) w = w / total;
-        if (lane < k) {
-            experts[t * k + lane] = mine;
-            weights[t * k + lane] = mine < 0 ? 0.f : w;
-            chosen[i * k + lane] = (int16_t)mine;
-            if (mine >= 0) atomicOr(&mask[i / 32][mine], 1u << (i % 32));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const int i = i0 + q;
+            if (i >= tokens) break;
+            const int64_t t = t0 + i;
+            const float b = of_key(best[q]);
+            float w = mine[q] < 0 ? 0.f : score == SPLITEE_SCORE_SOFTMAX ? expf(b - m[q]) : 1.0f / (1.0f + expf(-b));
+            const float sum = renorm ? wave_sum(w) : total[q];
+            if ((renorm || score == SPLITEE_SCORE_SOFTMAX) && sum != 0.f) w = w / sum;
+            if (lane < k) {
+                experts[t * k + lane] = mine[q];
+                weights[t * k + lane] = mine[q] < 0 ? 0.f : w;
+                chosen[i * k + lane] = (int16_t)mine[q];
+                if (mine[q] >= 0) atomicOr(&mask[i / 32][mine[q]], 1u << (i % 32));
+            }
         }
     }
     __syncthreads();
     __shared__ int off[ONE ? RT_MAX_E + 1 : 1];
-    auto rows_of = [&](int e) { return __popc(mask[0][e]) + __popc(mask[1][e]); };
+    auto rows_of = [&](int e) { return __popc(mask[0][e]) + (ONE ? __popc(mask[TOKENS / 32 - 1][e]) : 0); };
     if constexpr (ONE) {
         if (wave == 0) scan_experts(E, off, rows_of);
         __syncthreads();
@@ -166,8 +199,8 @@ route_topk_kernel(const float* __restrict__ logits, int64_t ldl, int T, int E, i
         int place = -1;
         if (e >= 0) {
             place = __popc(mask[i / 32][e] & ((1u << (i % 32)) - 1u));
-            if (i >= 32) place += __popc(mask[0][e]);
             if constexpr (ONE) {
+                if (i >= 32) place += __popc(mask[0][e]);
                 place += off[e];
                 row_index[place] = i;
             }
@@ -341,7 +374,7 @@ combine_kernel(const void* H, int64_t ldh, int64_t h_rows, const int32_t* __rest
 
 namespace splitee_host {
 
-// per workgroup of 64 tokens and expert one count, then the experts' totals
+// per workgroup and expert one count, then the experts' totals
 size_t route_workspace_bytes(int64_t T, int64_t E)
 {
     return (size_t)((T + RT_TOKENS - 1) / RT_TOKENS + 1) * (size_t)E * 4;
@@ -355,7 +388,7 @@ int launch_route(const float* logits, int64_t ldl, int64_t T, int64_t E, int64_t
         hipLaunchKernelGGL(route_empty_kernel, dim3(1), dim3(256), 0, s, offsets, (int)E);
         return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
     }
-    const int blocks = (int)((T + RT_TOKENS - 1) / RT_TOKENS);
+    const int blocks = T <= RT_ONE ? 1 : (int)((T + RT_TOKENS - 1) / RT_TOKENS);
     int32_t* counts = reinterpret_cast<int32_t*>(ws);
     int32_t* totals = counts + (int64_t)blocks * E;
 #define RT_RUN(V, ONE)                                                                                                \
