@@ -140,6 +140,22 @@ __device__ __forceinline__ void group_rows(const LinArgs& p, int e, int& begin, 
     end = min(max(p.offsets[e + 1], begin), p.rows);
 }
 
+// Inclusive sums over the lanes of the wave, by DPP.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int dpp_plus(int v)
+{
+    return v + __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_scan(int v)
+{
+    v = dpp_plus<0x111, 0xF>(v); // row_shr:1, 2, 4, 8
+    v = dpp_plus<0x112, 0xF>(v);
+    v = dpp_plus<0x114, 0xF>(v);
+    v = dpp_plus<0x118, 0xF>(v);
+    v = dpp_plus<0x142, 0xA>(v); // row_bcast:15, row_bcast:31
+    return dpp_plus<0x143, 0xC>(v);
+}
+
 // The group that holds row tile `at` of BM rows, the row tiles of all groups counted one group after
 // another, found by the whole wave: lanes take 64 groups at a time and scan their tile counts.  False where at
 // is past the last tile.  The offsets are read by every wave of a launch, a few hundred bytes from L2.
@@ -160,13 +176,7 @@ __device__ __forceinline__ bool find_group(const LinArgs& p, int at, Group& g)
         int begin = 0, end = 0;
         if (e0 + lane < p.experts) group_rows(p, e0 + lane, begin, end);
         const int tiles = (end - begin + BM - 1) / BM;
-        int incl = tiles;
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(incl, d, 64);
-            if (lane >= d) incl += up;
-        }
-        const int first = before + incl - tiles;
+        const int incl = wave_scan(tiles), first = before + incl - tiles;
         const uint64_t mine = __ballot(at >= first && at < first + tiles);
         if (mine) {
             const int src = __ffsll((unsigned long long)mine) - 1;

@@ -81,14 +81,6 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
     // Each is a buffer load from the tile's (of gathered rows: the matrix's) first row, its offset within the row
     // block fixed and the K tile in the scalar offset; an offset of 2 GB and more reads zeros.
     const int lchunk = (lane % 8) ^ ((4 * wave + lane / 16) & 7);
-    const uint16_t* const abase = reinterpret_cast<const uint16_t*>(p.A) + (p.row_index ? 0 : m0 * p.lda) + kt0 * BK;
-    constexpr int TPL = LA / NPL; // loads of a plane
-    uint32_t aoff[TPL];
-#pragma unroll
-    for (int t = 0; t < TPL; ++t) {
-        const int s = min(m0 + 8 * (wave + NW * t) + lane / 8, mend - 1); // a row past the group's: any of its rows
-        aoff[t] = (uint32_t)(((p.row_index ? splitee::a_row(p, s) : s - m0) * p.lda + lchunk * 8) * 2);
-    }
     // LDS row block b (32 weight rows) of the tile is column block b % TN of wave column b / TN; of a gated
     // tile the first TN / 2 are gate rows, the others the up rows of the same outputs
     const uint16_t* const wbase = reinterpret_cast<const uint16_t*>(p.W) + (int64_t)g.e * p.w_stride;
@@ -112,15 +104,27 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
     }
     unsigned char* const st[3] = {lt_stage<0, SB>(), lt_stage<1, SB>(), lt_stage<(S > 2 ? 2 : 0), SB>()};
     static_assert(S == 2 || S == 3, "stages");
-    // relative K tile t to the stage at `to`: zeros past K and past the split
-    auto issue = [&](int t, unsigned char* to) {
+    // the operands' relative K tile t to the stage at `to`: zeros past K and past the split
+    auto issue_w = [&](int t, unsigned char* to) {
         const int kleft = t < nk ? p.K - (kt0 + t) * BK : 0;
-        const uint32_t dead = lchunk * 8 < kleft ? 0u : OOB, wdead = TILED ? (kleft > 0 ? 0u : OOB) : dead;
+        const uint32_t dead = (TILED ? 0 : lchunk * 8) < kleft ? 0u : OOB;
+#pragma unroll
+        for (int i = 0; i < LW; ++i) lt_load(wb[i], woff[i] | dead, t * (TILED ? 4096 : BK * 2), to + AB + (wave + NW * i) * 1024);
+    };
+    issue_w(0, st[0]); // (ahead of the indexes of gathered rows)
+    const uint16_t* const abase = reinterpret_cast<const uint16_t*>(p.A) + (p.row_index ? 0 : m0 * p.lda) + kt0 * BK;
+    constexpr int TPL = LA / NPL; // loads of a plane
+    uint32_t aoff[TPL];
+#pragma unroll
+    for (int t = 0; t < TPL; ++t) {
+        const int s = min(m0 + 8 * (wave + NW * t) + lane / 8, mend - 1); // a row past the group's: any of its rows
+        aoff[t] = (uint32_t)(((p.row_index ? splitee::a_row(p, s) : s - m0) * p.lda + lchunk * 8) * 2);
+    }
+    auto issue_a = [&](int t, unsigned char* to) {
+        const uint32_t dead = lchunk * 8 < (t < nk ? p.K - (kt0 + t) * BK : 0) ? 0u : OOB;
 #pragma unroll
         for (int i = 0; i < LA; ++i)
             lt_load(abase + (i / TPL) * p.pstride, aoff[i % TPL] | dead, t * (BK * 2), to + (wave + NW * i) * 1024);
-#pragma unroll
-        for (int i = 0; i < LW; ++i) lt_load(wb[i], woff[i] | wdead, t * (TILED ? 4096 : BK * 2), to + AB + (wave + NW * i) * 1024);
     };
 
     f32x16_t acc[TM][TN];
@@ -182,7 +186,8 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         read(st[(c + 1) % S], 0, 0);
-        issue(t + S, st[c]);
+        issue_a(t + S, st[c]);
+        issue_w(t + S, st[c]);
         mul(1);
 #pragma unroll
         for (int i = 0; i < READS; ++i) {
@@ -198,8 +203,12 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
         __builtin_amdgcn_sched_barrier(0);
     };
 
+    issue_a(0, st[0]);
 #pragma unroll
-    for (int q = 0; q < S; ++q) issue(q, st[q]);
+    for (int q = 1; q < S; ++q) {
+        issue_a(q, st[q]);
+        issue_w(q, st[q]);
+    }
     wait_vmem<(S - 1) * (LA + LW)>();
     __builtin_amdgcn_s_barrier();
     read(st[0], 0, 0);
