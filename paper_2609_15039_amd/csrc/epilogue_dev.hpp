@@ -31,20 +31,36 @@ __device__ __forceinline__ float epi_logistic(float x)
 {
     return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * x));
 }
-__device__ __forceinline__ float epi_act(float z, int act)
+template <int ACT>
+__device__ __forceinline__ float epi_act1(float z)
 {
-    switch (act) {
-    case SPLITEE_ACT_SILU: return z * epi_logistic(z);
-    case SPLITEE_ACT_GELU: {
+    if (ACT == SPLITEE_ACT_SILU) return z * epi_logistic(z);
+    if (ACT == SPLITEE_ACT_GELU_TANH) return z * epi_logistic(1.59576912160573071f * (z + 0.044715f * z * z * z));
+    if (ACT == SPLITEE_ACT_RELU) return z < 0.0f ? 0.0f : z;
+    if (ACT == SPLITEE_ACT_GELU) {
         const float x = 0.70710678118654752f * fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
         const float q = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
         const float half = 0.5f * q * t * __builtin_amdgcn_exp2f(-1.44269504088896341f * x * x); // erfc(x) / 2
         return z < 0.0f ? z * half : z - z * half;
     }
-    case SPLITEE_ACT_GELU_TANH: return z * epi_logistic(1.59576912160573071f * (z + 0.044715f * z * z * z));
-    case SPLITEE_ACT_RELU: return z < 0.0f ? 0.0f : z;
-    default: return z;
+    return z;
+}
+// of n values, one choice for all
+template <int N>
+__device__ __forceinline__ void epi_act(float (&z)[N], int act)
+{
+#define EPI_CASE(A)                                             \
+    case A:                                                     \
+        _Pragma("unroll") for (int i = 0; i < N; ++i) z[i] = epi_act1<A>(z[i]); \
+        break
+    switch (act) {
+        EPI_CASE(SPLITEE_ACT_SILU);
+        EPI_CASE(SPLITEE_ACT_GELU);
+        EPI_CASE(SPLITEE_ACT_GELU_TANH);
+        EPI_CASE(SPLITEE_ACT_RELU);
+    default: break;
     }
+#undef EPI_CASE
 }
 
 // fl32(r - C) + bias of one element of the product: weight row n of group e, output row `row`
@@ -100,9 +116,9 @@ __device__ __forceinline__ void epi_finish4(const LinArgs& p, float4 z, float4 u
 {
     float h[4] = {z.x, z.y, z.z, z.w};
     const float u[4] = {up.x, up.y, up.z, up.w}, r[4] = {res.x, res.y, res.z, res.w};
+    epi_act(h, p.act);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        h[i] = epi_act(h[i], p.act);
         if (GATED) h[i] *= u[i];
         if (p.res) h[i] += r[i]; // (-0 stays -0 without one)
     }

@@ -172,7 +172,9 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
 #pragma unroll
             for (int v = 1; v < NW; ++v) z[h] += red[(v * BM + r) * LDR + h * BNO + c];
         }
-        float y = splitee::epi_act(splitee::epi_z(p, z[0], g.e, row, n), p.act);
+        float act[1] = {splitee::epi_z(p, z[0], g.e, row, n)};
+        splitee::epi_act(act, p.act);
+        float y = act[0];
         if (GATED) y *= splitee::epi_z(p, z[GATED ? 1 : 0], g.e, row, p.N + n);
         splitee::epi_store(p, y, row, n);
     }
