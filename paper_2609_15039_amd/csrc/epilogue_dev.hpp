@@ -82,69 +82,88 @@ __device__ __forceinline__ void epi_store(const LinArgs& p, float h, int row, in
     }
 }
 
-// Four columns of a row of the residual from column n on (left of them exist), zeros without one.
-__device__ __forceinline__ float4 epi_residual4(const LinArgs& p, int row, int n, int left)
+// N (4 or 8) columns of a row of the residual from column n on (left of them exist), zeros without one.
+template <int N>
+__device__ __forceinline__ void epi_residual(const LinArgs& p, int row, int n, int left, float (&r)[N])
 {
-    float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (!p.res) return r;
+#pragma unroll
+    for (int i = 0; i < N; ++i) r[i] = 0.f;
+    if (!p.res) return;
     const int64_t at = (int64_t)row * p.ldres + n;
     if (p.out_bf16) {
         const uint16_t* q = reinterpret_cast<const uint16_t*>(p.res) + at;
-        if (left >= 4) {
-            const uint2 v = *reinterpret_cast<const uint2*>(q);
-            return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xFFFF0000u), __uint_as_float(v.y << 16),
-                               __uint_as_float(v.y & 0xFFFF0000u));
+        if (left >= N) {
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) {
+                const uint2 v = reinterpret_cast<const uint2*>(q)[c];
+                r[4 * c] = __uint_as_float(v.x << 16);
+                r[4 * c + 1] = __uint_as_float(v.x & 0xFFFF0000u);
+                r[4 * c + 2] = __uint_as_float(v.y << 16);
+                r[4 * c + 3] = __uint_as_float(v.y & 0xFFFF0000u);
+            }
+            return;
         }
-        r.x = bf16_bits_to_f32(q[0]);
-        if (left > 1) r.y = bf16_bits_to_f32(q[1]);
-        if (left > 2) r.z = bf16_bits_to_f32(q[2]);
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) r[i] = bf16_bits_to_f32(q[i]);
     } else {
         const float* q = reinterpret_cast<const float*>(p.res) + at;
-        if (left >= 4) return *reinterpret_cast<const float4*>(q);
-        r.x = q[0];
-        if (left > 1) r.y = q[1];
-        if (left > 2) r.z = q[2];
+        if (left >= N) {
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) {
+                const f32x4_t v = reinterpret_cast<const f32x4_t*>(q)[c];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r[4 * c + i] = v[i];
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) r[i] = q[i];
     }
-    return r;
 }
 
-// The activation of four z of a row, the gate's product, the residual's sum and the store, from column n on; left:
-// columns that exist (4 and more: 16- or 8-byte stores).  STREAM: stores that do not stay in the L2, for results larger
-// than it (4096 x 4096 bfloat16: 2 us less).
-template <bool GATED, bool STREAM = false>
-__device__ __forceinline__ void epi_finish4(const LinArgs& p, float4 z, float4 up, float4 res, int row, int n, int left)
+// The activation of N (4 or 8) z of a row, the gate's product with up (gated), the residual's sum and the store, from
+// column n on; left: columns that exist (N and more: 8- or 16-byte stores).  STREAM: stores that do not stay in the L2, for
+// results larger than it (4096 x 4096 bfloat16: 2 us less).
+template <bool GATED, bool STREAM, int N>
+__device__ __forceinline__ void epi_finish(const LinArgs& p, float (&h)[N], const float (&up)[N], const float (&res)[N], int row, int n,
+                                           int left)
 {
-    float h[4] = {z.x, z.y, z.z, z.w};
-    const float u[4] = {up.x, up.y, up.z, up.w}, r[4] = {res.x, res.y, res.z, res.w};
     epi_act(h, p.act);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (GATED) h[i] *= u[i];
-        if (p.res) h[i] += r[i]; // (-0 stays -0 without one)
+    for (int i = 0; i < N; ++i) {
+        if (GATED) h[i] *= up[i];
+        if (p.res) h[i] += res[i]; // (-0 stays -0 without one)
     }
     const int64_t at = (int64_t)row * p.ldy + n;
     if (p.out_bf16) {
+        typedef uint32_t words_t __attribute__((ext_vector_type(N / 2)));
         uint16_t* y = reinterpret_cast<uint16_t*>(p.Y) + at;
-        const uint2 q = make_uint2(bf16x2_rne(h[0], h[1]), bf16x2_rne(h[2], h[3]));
-        if (left >= 4) {
-            const uint64_t v = (uint64_t)q.y << 32 | q.x;
-            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<uint64_t*>(y));
-            else *reinterpret_cast<uint64_t*>(y) = v;
+        words_t v;
+#pragma unroll
+        for (int i = 0; i < N / 2; ++i) v[i] = bf16x2_rne(h[2 * i], h[2 * i + 1]);
+        if (left >= N) {
+            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<words_t*>(y));
+            else *reinterpret_cast<words_t*>(y) = v;
         } else {
-            y[0] = (uint16_t)q.x;
-            if (left > 1) y[1] = (uint16_t)(q.x >> 16);
-            if (left > 2) y[2] = (uint16_t)q.y;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) y[i] = (uint16_t)(v[i / 2] >> (16 * (i % 2)));
         }
     } else {
         float* y = reinterpret_cast<float*>(p.Y) + at;
-        if (left >= 4) {
-            const f32x4_t v = {h[0], h[1], h[2], h[3]};
-            if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<f32x4_t*>(y));
-            else *reinterpret_cast<f32x4_t*>(y) = v;
+        if (left >= N) {
+#pragma unroll
+            for (int c = 0; c < N / 4; ++c) {
+                const f32x4_t v = {h[4 * c], h[4 * c + 1], h[4 * c + 2], h[4 * c + 3]};
+                if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<f32x4_t*>(y) + c);
+                else reinterpret_cast<f32x4_t*>(y)[c] = v;
+            }
         } else {
-            y[0] = h[0];
-            if (left > 1) y[1] = h[1];
-            if (left > 2) y[2] = h[2];
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < left) y[i] = h[i];
         }
     }
 }

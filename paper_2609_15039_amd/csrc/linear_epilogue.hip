@@ -33,9 +33,9 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinArgs p, const float*
         for (int i = 0; i < 4; ++i)
             if (n + i < p.N) z[h][i] = splitee::epi_z(p, z[h][i], 0, row, h * p.N + n + i);
     }
-    splitee::epi_finish4<GATED>(p, make_float4(z[0][0], z[0][1], z[0][2], z[0][3]),
-                                make_float4(z[GATED][0], z[GATED][1], z[GATED][2], z[GATED][3]),
-                                splitee::epi_residual4(p, row, n, p.N - n), row, n, p.N - n);
+    float res[4];
+    splitee::epi_residual(p, row, n, p.N - n, res);
+    splitee::epi_finish<GATED, false>(p, z[0], z[GATED], res, row, n, p.N - n);
 }
 
 }  // namespace

@@ -166,9 +166,9 @@ lin_f32_kernel(const LinArgs p, const int ntiles)
                 z[h][i] = zb[r * LD + 64 * h + c + i];
                 if (i < left) z[h][i] = splitee::epi_z(p, z[h][i], g.e, row, h * p.N + n + i);
             }
-        constexpr int U = TN - 1;
-        splitee::epi_finish4<GATED>(p, make_float4(z[0][0], z[0][1], z[0][2], z[0][3]), make_float4(z[U][0], z[U][1], z[U][2], z[U][3]),
-                                    splitee::epi_residual4(p, row, n, left), row, n, left);
+        float res[4];
+        splitee::epi_residual(p, row, n, left, res);
+        splitee::epi_finish<GATED, false>(p, z[0], z[TN - 1], res, row, n, left);
     }
 }
 

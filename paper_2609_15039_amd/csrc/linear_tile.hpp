@@ -254,10 +254,10 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
 #pragma unroll
     for (int q = 0; q < WGM; ++q)
         if (wm == q) zb = reinterpret_cast<float*>(st[q]);
-    // the activation and the stores take rows of the wave row's block, 4 columns a lane: up to 1 KB in a row
-    constexpr int BNO = T::BNO, LPR = BNO / 4, RPP = WAVE / LPR, RSTEP = WGN * RPP;
-    static_assert(LPR <= WAVE, "columns of a row");
-    const int pr = wn * RPP + lane / LPR, pc = lane % LPR * 4, n = n0 + pc;
+    // the activation and the stores take rows of the wave row's block, 8 columns a lane: whole rows of the tile
+    constexpr int BNO = T::BNO, CPL = 8, LPR = BNO / CPL, RPP = WAVE / LPR, RSTEP = WGN * RPP;
+    static_assert(LPR <= WAVE && RSTEP <= 32, "columns of a row");
+    const int pr = wn * RPP + lane / LPR, pc = lane % LPR * CPL, n = n0 + pc;
     const int left = p.N - n; // columns of the lane that exist
     // C of up to two row blocks of the wave ahead of both; elements outside load C[0].  (To wait for a load is to wait
     // for every store before it too.)
@@ -294,19 +294,33 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
                     p.bias ? acc[i][j][e] + bias[j] : acc[i][j][e];
         lt_barrier();
         const int rows_here = left > 0 ? min(32, mend - r0) : 0;
-        auto gate = [&](int r) { return *reinterpret_cast<const float4*>(zb + z_at(r, pc)); };
-        auto up = [&](int r) { return GATED ? *reinterpret_cast<const float4*>(zb + z_at(r, BNO + pc)) : make_float4(0.f, 0.f, 0.f, 0.f); };
+        auto finish = [&](int r, const float (&res)[CPL]) {
+            float z[CPL], u[CPL];
+#pragma unroll
+            for (int c = 0; c < CPL / 4; ++c) {
+                const f32x4_t a = *reinterpret_cast<const f32x4_t*>(zb + z_at(r, pc + 4 * c));
+                const f32x4_t b = GATED ? *reinterpret_cast<const f32x4_t*>(zb + z_at(r, BNO + pc + 4 * c)) : a;
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    z[4 * c + k] = a[k];
+                    u[4 * c + k] = b[k];
+                }
+            }
+            splitee::epi_finish<GATED, true>(p, z, u, res, r0 + r, n, left);
+        };
+        float res[CPL] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         if (!p.res) { // stores alone: with loads in the loop, each row would wait for the store before
 #pragma unroll 1
-            for (int r = pr; r < rows_here; r += RSTEP)
-                splitee::epi_finish4<GATED, true>(p, gate(r), up(r), make_float4(0.f, 0.f, 0.f, 0.f), r0 + r, n, left);
+            for (int r = pr; r < rows_here; r += RSTEP) finish(r, res);
         } else if (pr < rows_here) {
-            float4 res = splitee::epi_residual4(p, r0 + pr, n, left);
+            splitee::epi_residual(p, r0 + pr, n, left, res);
 #pragma unroll 1
             for (int r = pr; r < rows_here; r += RSTEP) {
-                const float4 next = splitee::epi_residual4(p, r0 + min(r + RSTEP, rows_here - 1), n, left);
-                splitee::epi_finish4<GATED, true>(p, gate(r), up(r), res, r0 + r, n, left);
-                res = next;
+                float next[CPL];
+                splitee::epi_residual(p, r0 + min(r + RSTEP, rows_here - 1), n, left, next);
+                finish(r, res);
+#pragma unroll
+                for (int k = 0; k < CPL; ++k) res[k] = next[k];
             }
         }
     }
