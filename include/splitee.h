@@ -359,7 +359,8 @@ size_t splitee_epilogue_workspace_bytes(int64_t M, int64_t N, int64_t K, int pre
  *   Y                   out, M x N of ep->out_type (ldy >= N), 16-byte aligned rows; must not overlap
  *                       anything else that is read, but may be the residual
  *   workspace           >= splitee_epilogue_workspace_bytes bytes, 256-byte aligned, no contents needed, none left
- * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^20 (SPLITEE_ERR_UNSUPPORTED above).
+ * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^20, N below 2^28
+ * (SPLITEE_ERR_UNSUPPORTED above).
  * Results do not depend on timing: repeated calls give the same bits.
  */
 int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void* W, int w_type, int64_t ldw,

@@ -721,6 +721,10 @@ def _epilogue(rows, N, NW, C, bias, act, gated, residual, out_dtype, bias_stride
     return ep
 
 
+def _tiled_elements(N, K):
+    return -(-N // 32) * -(-K // 64) * 2048
+
+
 def _out_width(NW, gated):
     _expect(not gated or NW % 2 == 0, "W: a gated projection has as many gate as up rows")
     return NW // 2 if gated else NW
@@ -735,6 +739,8 @@ def linear_epilogue(A, prec, W, C=None, bias=None, act="none", gated=False, resi
     _expect(len(W.shape) == 2 and W.shape[1] == K, "W: expected N x %d" % K)
     _expect(W.stride(1) == 1 or K <= 1, "W: columns are not contiguous")
     N = _out_width(NW, gated)
+    if isinstance(W, TiledWeights):
+        _expect(not M or W.data.numel() >= _tiled_elements(NW, K), "W: fewer elements than its tiled order has")
     dev = _here(A, W.data if isinstance(W, TiledWeights) else W, C, bias, residual, Y)
     if bias is not None:
         _expect(tuple(bias.shape) == (NW,) and bias.dtype == torch.float32 and (NW < 2 or bias.stride(0) == 1),
@@ -773,7 +779,7 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
                 "%s: expected contiguous int32%s" % (name, " of experts + 1" if n else ""))
     rows = a_rows if row_index is None else row_index.numel()
     if tiled:
-        _expect(W.data.dim() == 2 and W.data.shape[1] * 2 >= splitee_tiled_weights_bytes(NW, K) and W.data.stride(1) == 1,
+        _expect(W.data.dim() == 2 and W.data.shape[1] >= _tiled_elements(NW, K) and W.data.stride(1) == 1,
                 "W: expected experts x elements of tiled weights")
         ldw, w_stride = K, W.data.stride(0)
     else:

@@ -20,6 +20,7 @@ int launch_combine(const void* H, bool h_bf16, int64_t ldh, int64_t h_rows, cons
 namespace {
 
 constexpr int64_t LIN_MAX_LD = int64_t(1) << 20; // a tile's rows stay within 31 bits of its first one's address
+constexpr int64_t LIN_MAX_N = int64_t(1) << 28;
 constexpr int64_t ROUTE_MAX_E = 1024, ROUTE_MAX_K = 64;
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -69,7 +70,7 @@ extern "C" {
 size_t splitee_epilogue_workspace_bytes(int64_t M, int64_t N, int64_t K, int prec, int gated)
 {
     if (!valid_prec(prec) || !dims_ok(M, N, K) || K % 8 != 0 || gated < 0 || gated > 1) return 0;
-    if (M == 0 || N == 0) return 0;
+    if (M == 0 || N == 0 || N >= LIN_MAX_N || K >= LIN_MAX_LD) return 0;
     return splitee_host::linear_workspace_bytes(M, N, K, prec, gated);
 }
 
@@ -83,7 +84,8 @@ int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void*
     if (rc) return rc;
     rc = check_w(W, w_type, ldw, K, in_prec);
     if (rc) return rc;
-    if (lda >= LIN_MAX_LD || K >= LIN_MAX_LD || (w_type != SPLITEE_BF16_TILED && ldw >= LIN_MAX_LD)) return SPLITEE_ERR_UNSUPPORTED;
+    if (lda >= LIN_MAX_LD || K >= LIN_MAX_LD || N >= LIN_MAX_N || (w_type != SPLITEE_BF16_TILED && ldw >= LIN_MAX_LD))
+        return SPLITEE_ERR_UNSUPPORTED;
     const size_t need = splitee_epilogue_workspace_bytes(M, N, K, in_prec, ep->gated);
     if (workspace_bytes < need || (need > 0 && workspace == nullptr)) return SPLITEE_ERR_WORKSPACE;
     if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return SPLITEE_ERR_ALIGN;
@@ -108,7 +110,8 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
     if (rc) return rc;
     rc = check_w(W, w_type, ldw, K, in_prec);
     if (rc) return rc;
-    if (lda >= LIN_MAX_LD || K >= LIN_MAX_LD || (w_type != SPLITEE_BF16_TILED && ldw >= LIN_MAX_LD)) return SPLITEE_ERR_UNSUPPORTED;
+    if (lda >= LIN_MAX_LD || K >= LIN_MAX_LD || N >= LIN_MAX_N || (w_type != SPLITEE_BF16_TILED && ldw >= LIN_MAX_LD))
+        return SPLITEE_ERR_UNSUPPORTED;
     // gathered rows are addressed from the first one's with 31 bits
     if (row_index && a_rows * lda * prec_elsize(in_prec) > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
     if (!pitch16(w_stride, w_type == SPLITEE_F32 ? 4 : 2)) return SPLITEE_ERR_ALIGN;

@@ -48,7 +48,7 @@ COMMON = [(dict(prec=PD), UNSUP), (dict(prec=9), UNSUP), (dict(ep=False), ARG), 
           (dict(w_type=5), DTYPE), (dict(w_type=F32), UNSUP), (dict(w_type=TILED, prec=PF), UNSUP), (dict(A=None), ARG),
           (dict(W=None), ARG), (dict(Y=None), ARG), (dict(A=8), ALIGN), (dict(W=8), ALIGN), (dict(Y=8), ALIGN), (dict(lda=36), ALIGN),
           (dict(ldw=36), ALIGN), (dict(ldy=18), ALIGN), (dict(lda=BIG), UNSUP), (dict(ldw=BIG), UNSUP),
-          (dict(w_type=TILED, K=BIG, lda=BIG), UNSUP), (dict(N=0), OK)]
+          (dict(w_type=TILED, K=BIG, lda=BIG), UNSUP), (dict(N=1 << 28, ldy=1 << 28), UNSUP), (dict(N=0), OK)]
 
 
 @pytest.mark.parametrize("kw,code", COMMON + [(dict(M=-1), SHAPE), (dict(M=0), OK), (dict(ws=128), ALIGN)])
@@ -132,6 +132,8 @@ def test_binding_refuses_what_the_library_cannot_see():
         sp.linear_epilogue(A, sp.SPLITEE_PREC_BF16, W[:, :24])
     with pytest.raises(ValueError, match="gated"):
         sp.linear_epilogue(A, sp.SPLITEE_PREC_BF16, W[:15], gated=True)
+    with pytest.raises(ValueError, match="tiled"):
+        sp.linear_epilogue(A, sp.SPLITEE_PREC_BF16, sp.TiledWeights(torch.zeros(2047, dtype=torch.bfloat16), 16, 32))
     with pytest.raises(ValueError, match="experts"):
         sp.grouped_linear(A, sp.SPLITEE_PREC_BF16, W, torch.zeros(3, dtype=torch.int32))
     with pytest.raises(ValueError, match="logits"):
