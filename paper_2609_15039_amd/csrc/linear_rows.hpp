@@ -3,7 +3,7 @@
 // Bound by W, read once from HBM.  A workgroup owns BM rows (8, 16 or 32) and 16 TN weight rows (gated: half of
 // them gate, half up rows of the same outputs); its waves split K: wave w takes the 64-k tiles w, w + NW, ..,
 // and the waves' sums meet in LDS and are added in wave order, so that the result does not depend on timing and
-// no other workgroup is waited for.  W goes straight to the registers that the MFMA reads, R K tiles ahead; the rows
+// no other workgroup is waited for.  W goes straight to the registers that the MFMA reads, two K tiles ahead; the rows
 // of A go to LDS by 1 KB loads, 8 rows of whole 128-byte lines each, into a stage that belongs to one
 // wave: no barrier in the loop.  Two K tiles ahead: three and four were slower (one token of 2 x 9728 x 2560 17.6, 21.8 and
 // 23.7 us, W then partly in caches), and so were 32-row tiles (32 rows in three planes 34 us, twice 16 rows 33).
@@ -29,10 +29,11 @@ __device__ __forceinline__ uint4 lr_load(const void* base, uint32_t voff, int so
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 
-template <int NPL, int BM, int TN, int NW, int R, bool GATED, bool TILED>
+template <int NPL, int BM, int TN, int NW, bool GATED, bool TILED>
 __global__ void __launch_bounds__(NW * WAVE)
 lin_rows_kernel(const LinArgs p, const int ntiles)
 {
+    constexpr int R = 2;                        // K tiles ahead
     constexpr int MT = (BM + 15) / 16;          // 16-row blocks of the MFMA
     constexpr int LA = NPL * BM / 8, LW = 2 * TN; // loads per K tile
     constexpr int TO = GATED ? TN / 2 : TN, BN = 16 * TN, BNO = 16 * TO;
@@ -84,8 +85,7 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
         const int s = min(m0 + 8 * t + lane / 8, g.end - 1);
         aoff[t] = (uint32_t)((p.row_index ? splitee::a_row(p, s) : s - m0) * p.lda * 2);
     }
-    unsigned char* const st[4] = {lr_stage<0, NW * SBP>(), lr_stage<1, NW * SBP>(), lr_stage<(R > 2 ? 2 : 0), NW * SBP>(),
-                                  lr_stage<(R > 3 ? 3 : 0), NW * SBP>()};
+    unsigned char* const st[R] = {lr_stage<0, NW * SBP>(), lr_stage<1, NW * SBP>()};
     uint4 wr[R][2][TN];
     // this wave's K tile gk into ring slot u (zeros past its last)
     auto issue = [&](int gk, int u) {
@@ -141,19 +141,19 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
     for (; gk + R <= ng; gk += R) {
 #pragma unroll
         for (int u = 0; u < R; ++u) {
-            wait_vmem<(R - 1) * (LA + LW)>(); // this slot's loads are in; the younger slots' may be in flight
+            wait_vmem<(R - 1) * (LA + LW)>(); // this slot's loads are in; the younger slot's may be in flight
+            __builtin_amdgcn_sched_barrier(0);
             consume(u);
             __builtin_amdgcn_s_waitcnt((0 << 8) | (7 << 4) | 15 | (3 << 14)); // lgkmcnt(0): the slot's rows are read
             issue(gk + u + R, u);
         }
     }
-    wait_vmem<0>(); // the last tiles, and the loads past them (zeros)
-#pragma unroll
-    for (int u = 0; u < R - 1; ++u)
-        if (gk + u < ng) consume(u);
+    wait_vmem<0>(); // the last tile of an odd count, and the loads past it (zeros)
+    __builtin_amdgcn_sched_barrier(0);
+    if (gk < ng) consume(0);
 
     // the waves' sums meet in LDS and are added in wave order
-    float* const red = reinterpret_cast<float*>(RB <= NW * SBP ? st[0] : lr_stage<4, RB <= NW * SBP ? 16 : RB>());
+    float* const red = reinterpret_cast<float*>(RB <= NW * SBP ? st[0] : lr_stage<2, RB <= NW * SBP ? 16 : RB>());
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < MT; ++i)

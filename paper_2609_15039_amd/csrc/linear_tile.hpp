@@ -220,6 +220,7 @@ __device__ __forceinline__ void lin_tile(const LinArgs& p, const LtPlan& plan, c
     }
     wait_vmem<(S - 1) * (LA + LW)>();
     __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
     read(st[0], 0, 0);
     int t = 0;
     for (; t + S <= nk; t += S) {
