@@ -802,10 +802,12 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
 
 def tile_experts(W):
     """experts x N x K bfloat16 in the tiled order, an expert a row of the TiledWeights' data."""
+    _expect(W.dim() == 3 and W.dtype == torch.bfloat16 and (W.stride(2) == 1 or W.shape[2] <= 1),
+            "W: expected bfloat16 of experts x N x K, columns contiguous")
     E, N, K = W.shape
     data = torch.empty((E, splitee_tiled_weights_bytes(N, K) // 2), dtype=torch.bfloat16, device=W.device)
     for e in range(E):
-        splitee_tile_weights(W[e], W.stride(1), N, K, data[e])
+        splitee_tile_weights(W[e], W.stride(1) if N > 1 else K, N, K, data[e])
     return TiledWeights(data, N, K)
 
 
@@ -866,7 +868,7 @@ def _mask_planes(X, rows, K, prec, mech, sensitivity, epsilon, seed, stream_id, 
     """noise_mask of X, or (X None) of zeros: the planes of the mask itself."""
     planes = 3 if prec == SPLITEE_PREC_BF16X3 else 1
     Xt = torch.empty((planes, rows, K), dtype=torch.float32 if prec == SPLITEE_PREC_F32 else torch.int16, device=device)
-    splitee_noise_mask(X, K if X is None else X.stride(0), Xt, prec, K, rows, K, mech, sensitivity, epsilon, seed, stream_id, row0)
+    splitee_noise_mask(X, K if X is None or rows < 2 else X.stride(0), Xt, prec, K, rows, K, mech, sensitivity, epsilon, seed, stream_id, row0)
     return Xt
 
 
@@ -883,8 +885,15 @@ def expert_ffn(X, logits, k, W_gate_up, W_down, mech=SPLITEE_MECH_NONE, sensitiv
     row0 k .. of stream stream_id + 1 (down: one for each row in the router's order).  As in the fused call the
     corrections are formed on this GPU, here once the rows' experts are known; SPLITEE_MECH_NONE is the split without
     noise, which has none."""
+    _expect(X.dim() == 2 and X.dtype == torch.float32 and (X.stride(1) == 1 or X.shape[1] <= 1),
+            "X: expected float32 of tokens x K, columns contiguous")
     T, K = X.shape
-    N = W_down.shape[-1]
+    D, N = W_down.shape[-2:]
+    _expect(logits.dim() == 2 and logits.shape[0] == T, "logits: expected %d tokens x experts" % T)
+    _expect(tuple(W_gate_up.shape[-2:]) == (2 * N, K), "W_gate_up: expected experts x %d x %d" % (2 * N, K))
+    if residual is not None:
+        _matrix("residual", residual, (T, D), out_dtype)
+    _here(X, logits, residual, *(W.data if isinstance(W, TiledWeights) else W for W in (W_gate_up, W_down)))
     r = route(logits, k, score=score, renorm=renorm)
     noise_args = (mech, sensitivity, epsilon, seed)
     masked = mech != SPLITEE_MECH_NONE

@@ -140,3 +140,29 @@ def test_binding_refuses_what_the_library_cannot_see():
         sp.route(A, 2)
     with pytest.raises(ValueError, match="slot"):
         sp.combine(A, torch.zeros(4, 2), torch.zeros(4, 2))
+
+
+def ffn_arguments(**kw):
+    a = dict(X=torch.zeros(6, 32), logits=torch.zeros(6, 4), k=2, W_gate_up=torch.zeros(4, 48, 32, dtype=torch.bfloat16),
+             W_down=torch.zeros(4, 16, 24, dtype=torch.bfloat16))
+    a.update(kw)
+    return a
+
+
+@pytest.mark.parametrize("kw,match", [
+    (dict(X=torch.zeros(6, 32, dtype=torch.bfloat16)), "X:"), (dict(X=torch.zeros(2, 6, 32)), "X:"),
+    (dict(X=torch.zeros(32, 6).t()), "X:"), (dict(logits=torch.zeros(5, 4)), "logits:"), (dict(logits=torch.zeros(6)), "logits:"),
+    (dict(W_gate_up=torch.zeros(4, 48, 24, dtype=torch.bfloat16)), "W_gate_up:"),
+    (dict(W_gate_up=torch.zeros(4, 42, 32, dtype=torch.bfloat16)), "W_gate_up:"),  # 21 outputs, whose rows are 24 apart
+    (dict(W_gate_up=torch.zeros(4, 24, 32, dtype=torch.bfloat16)), "W_gate_up:"),
+    (dict(residual=torch.zeros(5, 16)), "residual:"), (dict(residual=torch.zeros(6, 16, dtype=torch.bfloat16)), "residual:")])
+def test_expert_ffn_refuses_before_anything_runs(kw, match):
+    with pytest.raises(ValueError, match=match):
+        sp.expert_ffn(**ffn_arguments(**kw))
+
+
+@pytest.mark.parametrize("W", [torch.zeros(2, 32, 64), torch.zeros(32, 64, dtype=torch.bfloat16),
+                               torch.zeros(2, 64, 32, dtype=torch.bfloat16).transpose(1, 2)])
+def test_tile_experts_refuses(W):
+    with pytest.raises(ValueError, match="W:"):
+        sp.tile_experts(W)
