@@ -41,7 +41,7 @@ __device__ __forceinline__ float epi_act1(float z)
         const float x = 0.70710678118654752f * fabsf(z), t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, x, 1.0f));
         const float q = fmaf(fmaf(fmaf(fmaf(1.061405429f, t, -1.453152027f), t, 1.421413741f), t, -0.284496736f), t, 0.254829592f);
         const float half = 0.5f * q * t * __builtin_amdgcn_exp2f(-1.44269504088896341f * x * x); // erfc(x) / 2
-        return z < 0.0f ? z * half : z - z * half;
+        return z * (z < 0.0f ? half : 1.0f - half); // (z - z half would make +inf a NaN)
     }
     return z;
 }

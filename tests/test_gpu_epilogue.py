@@ -128,6 +128,26 @@ def test_infinities_and_nan_stay_in_their_row(M, prec, layout):
     assert torch.isinf(Y[0]).all() and torch.isnan(Y[M - 1]).all()
 
 
+@pytest.mark.parametrize("act", list(sp.ACTS))
+@pytest.mark.parametrize("prec,layout", KINDS)
+@pytest.mark.parametrize("M", [1, 40, 400])
+def test_activations_at_the_ends_of_the_range(M, prec, layout, act):
+    """A product of zeros, so that z is the bias: infinities, NaN and values whose squares or cubes overflow give what
+    the formula gives (+inf stays +inf, -inf is 0 of a ReLU and else NaN), the others 16 u of |z|."""
+    inf, low = float("inf"), torch.finfo(F32).min
+    z = torch.tensor([inf, -inf, float("nan"), -low, low, 1e20, -1e20, 1e13, -1e13, 100.0, -100.0, 20.0, -20.0, 5.0, -5.0, 0.0, 1e-30])
+    z = z.repeat(11)
+    W = weights(torch.ones(z.numel(), 64), layout)
+    Y = sp.linear_epilogue(R.split(torch.zeros(M, 64), prec).to(DEV), sp.PRECS[prec], W, bias=z.to(DEV), act=act).cpu().double()
+    want = R.act64(z.double(), act).expand(M, -1)
+    assert torch.equal(torch.isnan(Y), torch.isnan(want))
+    ends = torch.isinf(want)
+    assert torch.equal(Y[ends], want[ends])
+    rest = ~ends & ~torch.isnan(want)
+    bound = 16 * R.U * z.double().abs().expand(M, -1) + torch.finfo(F32).tiny
+    assert ((Y - want)[rest].abs() <= bound[rest]).all()
+
+
 @pytest.mark.parametrize("M,N,K,prec", [(2, 512, 2560, "bf16x3"), (60, 256, 4096, "bf16"), (300, 640, 2048, "bf16x3")])
 def test_residual_in_place(M, N, K, prec):
     X, W, res = ints((M, K), -8, 8, 1), ints((N, K), -4, 4, 2), ints((M, N), -99, 99, 3)
