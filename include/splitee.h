@@ -359,8 +359,8 @@ size_t splitee_epilogue_workspace_bytes(int64_t M, int64_t N, int64_t K, int pre
  *   Y                   out, M x N of ep->out_type (ldy >= N), 16-byte aligned rows; must not overlap
  *                       anything else that is read, but may be the residual
  *   workspace           >= splitee_epilogue_workspace_bytes bytes, 256-byte aligned, no contents needed, none left
- * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^20, N below 2^28
- * (SPLITEE_ERR_UNSUPPORTED above).
+ * K % 8 == 0; K == 0 is a product of zeros.  lda, ldw and K below 2^20, N below 2^28, and no more
+ * tiles than a launch takes, 2^32 threads (SPLITEE_ERR_UNSUPPORTED above).
  * Results do not depend on timing: repeated calls give the same bits.
  */
 int splitee_linear_epilogue(const void* A, int in_prec, int64_t lda, const void* W, int w_type, int64_t ldw,
@@ -404,7 +404,7 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
  *   row_index   out, T * k int32: the token of each row; -1 from offsets[E] on
  *   slot        out, T x k int32: the row of (token, choice); -1 beside -1
  * experts, weights and slot are dense (leading dimension k).  1 <= k <= min(E, 64), E <= 1024
- * (SPLITEE_ERR_UNSUPPORTED above), T k < 2^31.  T == 0 writes zero offsets.  workspace: >=
+ * T <= 2^26, T k < 2^31 (SPLITEE_ERR_UNSUPPORTED above).  T == 0 writes zero offsets.  workspace: >=
  * splitee_route_workspace_bytes bytes, 256-byte aligned, no contents needed.
  */
 typedef enum { SPLITEE_SCORE_SOFTMAX = 0, SPLITEE_SCORE_SIGMOID = 1 } splitee_score;
@@ -421,7 +421,7 @@ int splitee_route(const float* logits, int64_t ldl, int64_t T, int64_t E, int64_
  *   weights     device, T x k float32 (dense)
  *   residual    T x N of out_type (ldres) or NULL; may be Y itself (same leading dimension)
  *   Y           out, T x N of out_type, leading dimension ldy; must not overlap H
- * 1 <= k <= 64, N below 2^20 (SPLITEE_ERR_UNSUPPORTED above).
+ * 1 <= k <= 64, N below 2^20, T below 2^24 (SPLITEE_ERR_UNSUPPORTED above).
  */
 int splitee_combine(const void* H, int h_type, int64_t ldh, int64_t h_rows, const int32_t* slot, const float* weights,
                     const void* residual, int64_t ldres, void* Y, int out_type, int64_t ldy, int64_t T, int64_t k,

@@ -868,7 +868,8 @@ def _mask_planes(X, rows, K, prec, mech, sensitivity, epsilon, seed, stream_id, 
     """noise_mask of X, or (X None) of zeros: the planes of the mask itself."""
     planes = 3 if prec == SPLITEE_PREC_BF16X3 else 1
     Xt = torch.empty((planes, rows, K), dtype=torch.float32 if prec == SPLITEE_PREC_F32 else torch.int16, device=device)
-    splitee_noise_mask(X, K if X is None or rows < 2 else X.stride(0), Xt, prec, K, rows, K, mech, sensitivity, epsilon, seed, stream_id, row0)
+    splitee_noise_mask(X, K if X is None or rows < 2 else X.stride(0), Xt, prec, K, rows, K, mech, sensitivity, epsilon, seed,
+                       stream_id, row0)
     return Xt
 
 

@@ -22,6 +22,8 @@ namespace {
 constexpr int64_t LIN_MAX_LD = int64_t(1) << 20; // a tile's rows stay within 31 bits of its first one's address
 constexpr int64_t LIN_MAX_N = int64_t(1) << 28;
 constexpr int64_t ROUTE_MAX_E = 1024, ROUTE_MAX_K = 64;
+// tokens: a launch has fewer than 2^32 threads (32 a token in the router, 256 in the weighted sum)
+constexpr int64_t ROUTE_MAX_T = int64_t(1) << 26, COMBINE_MAX_T = (int64_t(1) << 24) - 1;
 
 inline bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 inline bool valid_out(int t) { return t == SPLITEE_F32 || t == SPLITEE_BF16; }
@@ -146,7 +148,7 @@ int splitee_linear_plan_probe(int64_t rows, int64_t groups, int dense, int64_t N
 
 size_t splitee_route_workspace_bytes(int64_t T, int64_t E, int64_t k)
 {
-    if (!dims_ok(T, E, k) || k < 1 || k > E || k > ROUTE_MAX_K || E > ROUTE_MAX_E || T * k > INT32_MAX) return 0;
+    if (!dims_ok(T, E, k) || k < 1 || k > E || k > ROUTE_MAX_K || E > ROUTE_MAX_E || T > ROUTE_MAX_T || T * k > INT32_MAX) return 0;
     return splitee_host::route_workspace_bytes(T, E);
 }
 
@@ -156,7 +158,7 @@ int splitee_route(const float* logits, int64_t ldl, int64_t T, int64_t E, int64_
 {
     if (score != SPLITEE_SCORE_SOFTMAX && score != SPLITEE_SCORE_SIGMOID) return SPLITEE_ERR_ARG;
     if (!dims_ok(T, E, k) || k < 1 || k > E || ldl < E) return SPLITEE_ERR_SHAPE;
-    if (E > ROUTE_MAX_E || k > ROUTE_MAX_K || T * k > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
+    if (E > ROUTE_MAX_E || k > ROUTE_MAX_K || T > ROUTE_MAX_T || T * k > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
     const size_t need = splitee_host::route_workspace_bytes(T, E);
     if (!workspace || workspace_bytes < need) return SPLITEE_ERR_WORKSPACE;
     if (reinterpret_cast<uintptr_t>(workspace) & 255u) return SPLITEE_ERR_ALIGN;
@@ -174,7 +176,7 @@ int splitee_combine(const void* H, int h_type, int64_t ldh, int64_t h_rows, cons
 {
     if (!valid_out(h_type) || !valid_out(out_type)) return SPLITEE_ERR_DTYPE;
     if (!dims_ok(T, N, k) || !dims_ok(h_rows, 0, 0) || k < 1 || ldh < N || ldy < N || (residual && ldres < N)) return SPLITEE_ERR_SHAPE;
-    if (k > ROUTE_MAX_K || N >= LIN_MAX_LD) return SPLITEE_ERR_UNSUPPORTED;
+    if (k > ROUTE_MAX_K || N >= LIN_MAX_LD || T > COMBINE_MAX_T) return SPLITEE_ERR_UNSUPPORTED;
     if (T == 0 || N == 0) return SPLITEE_OK;
     if ((!H && h_rows > 0) || !slot || !weights || !Y) return SPLITEE_ERR_ARG;
     if (!aligned16(H) || !pitch16(ldh, out_elsize(h_type)) || !aligned16(Y) || !pitch16(ldy, out_elsize(out_type)) ||

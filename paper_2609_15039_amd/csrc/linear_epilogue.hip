@@ -125,12 +125,12 @@ F32Dense f32_dense(int64_t M, int64_t N, int64_t K, int gated)
     return d;
 }
 
+int64_t sum_workgroups(const LinArgs& p) { return ((int64_t)p.rows * ((p.N + 3) / 4) + 255) / 256; }
+
 int launch_sum(const LinArgs& p, const float* part, int ksplit, hipStream_t s)
 {
-    const int64_t quads = (int64_t)p.rows * ((p.N + 3) / 4);
     const int ld = (int)part_ld(p.N, p.gated);
-    if ((quads + 255) / 256 > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
-    const dim3 grid((unsigned)((quads + 255) / 256));
+    const dim3 grid((unsigned)sum_workgroups(p));
     if (p.gated) hipLaunchKernelGGL(linear_sum_kernel<true>, grid, dim3(256), 0, s, p, part, ksplit, ld);
     else hipLaunchKernelGGL(linear_sum_kernel<false>, grid, dim3(256), 0, s, p, part, ksplit, ld);
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
@@ -138,6 +138,7 @@ int launch_sum(const LinArgs& p, const float* part, int ksplit, hipStream_t s)
 
 int launch_dense_f32(const LinArgs& p, int w_type, void* ws, hipStream_t s)
 {
+    if (!launch_fits(sum_workgroups(p), 256)) return SPLITEE_ERR_UNSUPPORTED;
     const F32Dense d = f32_dense(p.rows, p.N, p.K, p.gated);
     const float* A = reinterpret_cast<const float*>(p.A);
     if (!p.gated && !p.bias && !p.res && p.act == SPLITEE_ACT_NONE && !p.out_bf16) // the unmask is the GEMM's own
@@ -170,6 +171,7 @@ int launch_linear(const LinArgs& p, int prec, int w_type, void* ws, hipStream_t 
     if (plan.kind == LinPlan::ROWS)
         return x3 ? launch_linear_rows_bf16x3(p, tiled, plan, s) : launch_linear_rows_bf16(p, tiled, plan, s);
     float* part = plan.ksplit > 1 ? reinterpret_cast<float*>(ws) : nullptr;
+    if (part && !launch_fits(sum_workgroups(p), 256)) return SPLITEE_ERR_UNSUPPORTED;
     const int rc = x3 ? launch_linear_tile_bf16x3(p, tiled, plan, part, s) : launch_linear_tile_bf16(p, tiled, plan, part, s);
     return rc != SPLITEE_OK || !part ? rc : launch_sum(p, part, plan.ksplit, s);
 }

@@ -176,7 +176,7 @@ template <int TM, bool GATED>
 int f32_run(const LinArgs& p, bool bf16, hipStream_t s)
 {
     const int64_t nt = (p.N + 63) / 64, wgs = (p.rows / (16 * TM) + (int64_t)p.experts) * nt;
-    if (wgs > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
+    if (!splitee_host::launch_fits(wgs, LF_NT)) return SPLITEE_ERR_UNSUPPORTED;
     if (bf16) hipLaunchKernelGGL((lin_f32_kernel<TM, GATED, true>), dim3((unsigned)wgs), dim3(LF_NT), 0, s, p, (int)nt);
     else hipLaunchKernelGGL((lin_f32_kernel<TM, GATED, false>), dim3((unsigned)wgs), dim3(LF_NT), 0, s, p, (int)nt);
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;

@@ -26,4 +26,7 @@ int launch_grouped_f32(const splitee::LinArgs& p, bool w_bf16, hipStream_t s);
 // Leading dimension of a split's partial product (16-byte rows; of a gated one, gate columns then up columns).
 inline int64_t part_ld(int64_t N, int gated) { return (N + 3) / 4 * 4 * (gated ? 2 : 1); }
 
+// A launch has fewer than 2^32 threads.
+inline bool launch_fits(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 }  // namespace splitee_host

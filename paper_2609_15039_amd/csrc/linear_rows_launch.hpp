@@ -11,7 +11,7 @@ int rows_run(const LinArgs& p, hipStream_t s)
     constexpr int BNO = 16 * (GATED ? TN / 2 : TN);
     const int64_t nt = (p.N + BNO - 1) / BNO;
     const int64_t strips = p.offsets ? p.rows / BM + (int64_t)p.experts : (p.rows + BM - 1) / BM;
-    if (strips * nt > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
+    if (!splitee_host::launch_fits(strips * nt, NW * WAVE)) return SPLITEE_ERR_UNSUPPORTED;
     hipLaunchKernelGGL((lin_rows_kernel<NPL, BM, TN, NW, GATED, TILED>), dim3((unsigned)(strips * nt)), dim3(NW * WAVE), 0, s, p,
                        (int)nt);
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;

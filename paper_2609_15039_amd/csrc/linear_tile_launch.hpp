@@ -14,7 +14,7 @@ int tile_run(const LinArgs& p, const splitee_host::LinPlan& plan, float* part, h
     const int64_t tiles = strips * nt, nbig = HALF && plan.halve ? tiles / 256 * 256 : tiles;
     const int64_t wgs = p.offsets ? (tiles + 255) / 256 * 256 // (by expert: the 8 x 32 order)
                                   : (nbig + 2 * (tiles - nbig)) * plan.ksplit;
-    if (wgs > INT32_MAX) return SPLITEE_ERR_UNSUPPORTED;
+    if (!splitee_host::launch_fits(wgs, T::NT)) return SPLITEE_ERR_UNSUPPORTED;
     const LtPlan lt{(int)nt, plan.ksplit, plan.ktps, part, (int)splitee_host::part_ld(p.N, GATED), (int)(2 * (tiles - nbig))};
     hipLaunchKernelGGL((lin_tile_kernel<NPL, BM, BN, WGM, WGN, S, GATED, TILED, HALF>), dim3((unsigned)wgs), dim3(T::NT), 0, s, p, lt);
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;

@@ -117,6 +117,23 @@ def test_combine_validation(lib, kw, code):
     assert combine(lib, **kw) == code
 
 
+GB = 1 << 30
+
+
+@pytest.mark.parametrize("call", [
+    lambda lib: linear(lib, M=GB, N=1 << 20, K=8, ldy=1 << 20, nbytes=1 << 62),
+    lambda lib: linear(lib, epilogue(act=1), prec=PF, M=1 << 22, N=1 << 20, K=8, ldy=1 << 20, nbytes=1 << 62),
+    lambda lib: linear(lib, prec=PF, M=1 << 22, N=1 << 20, K=8, ldy=1 << 20, nbytes=1 << 62),
+    lambda lib: grouped(lib, experts=GB, N=1 << 20, ldy=1 << 20),
+    lambda lib: grouped(lib, prec=PX, experts=GB, N=1 << 20, ldy=1 << 20),
+    lambda lib: grouped(lib, prec=PF, experts=GB, N=1 << 20, ldy=1 << 20),
+    lambda lib: route(lib, T=(1 << 26) + 1, E=1, k=1, ldl=1),
+    lambda lib: combine(lib, T=1 << 24)])
+def test_more_than_a_launch_takes_is_refused(lib, call):
+    """2^32 threads and more: refused before the launch, of which the device would say an error."""
+    assert call(lib) == UNSUP
+
+
 def test_binding_refuses_what_the_library_cannot_see():
     """Shapes and types of tensors, and tensors that are not on the device (none is here)."""
     A, W = torch.zeros(4, 32, dtype=torch.bfloat16), torch.zeros(16, 32, dtype=torch.bfloat16)
