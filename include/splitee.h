@@ -394,7 +394,8 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
  * Router of a mixture-of-experts layer: the k experts of each token, their weights, and the order of rows
  * that splitee_grouped_linear and splitee_combine take.
  *   logits      T x E float32, leading dimension ldl >= E (4-byte aligned).  A logit of -inf or NaN masks its
- *               expert: it is not chosen, and its score is 0
+ *               expert: it is not chosen, and its score is 0.  +inf is chosen first, in a SOFTMAX with NaN for
+ *               the token's weights, as the formula says (a SIGMOID's is 1)
  *   score       SOFTMAX: exp(l - max l) / sum over the row's experts; SIGMOID: 1 / (1 + exp(-l))
  *   renorm      != 0: the chosen weights are divided by their sum (left 0 where that is 0)
  *   experts     out, T x k int32: the k largest logits in falling order, equal ones by rising index;

@@ -57,6 +57,22 @@ def test_ties_and_masks(T, E, k, score):
         assert (r.experts[::7] == -1).all() and (r.weights[::7] == 0).all() and (r.slot[::7] == -1).all()
 
 
+@pytest.mark.parametrize("T", [3, 100])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_infinite_logits(T, renorm):
+    """+inf before every number, two of them by index; softmax weights NaN, a sigmoid's 1; tokens beside it as ever."""
+    L = torch.arange(20.0).repeat(T, 1) / 8
+    L[0, 5] = L[0, 11] = float("inf")
+    L[0, 2] = float("nan")
+    other = R.route_ref(L[1:], 3, "softmax", renorm)[1]
+    r = sp.route(L.to(DEV), 3, renorm=renorm)
+    assert r.experts[0].tolist() == [5, 11, 19] and torch.isnan(r.weights[0]).all()
+    bound = (88 + 4 + 20 + 4) * R.U * other + 1e-37  # as in check
+    assert (np.abs(r.weights[1:].cpu().numpy() - other) <= bound).all()
+    s = sp.route(L.to(DEV), 3, score="sigmoid", renorm=False)
+    assert s.experts[0].tolist() == [5, 11, 19] and s.weights[0, :2].tolist() == [1.0, 1.0]
+
+
 def test_no_tokens_and_all_masked():
     r = sp.route(torch.empty((0, 9), device=DEV), 3)
     assert torch.equal(r.offsets.cpu(), torch.zeros(10, dtype=torch.int32))
