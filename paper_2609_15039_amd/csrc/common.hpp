@@ -113,8 +113,16 @@ int launch_product(const void* A, int prec, int64_t lda, int64_t plane_stride, c
                    float* Out, int64_t ldo, int64_t M, int64_t N, int64_t K, hipStream_t s);
 // Binary32 GEMM, A float32, W row-major float32 or bfloat16; ws null: K is not split.
 size_t f32_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K);
+// Partial tiles of a binary32 product whose tiles are all split: split q of tile t (tm 16-row blocks x 64 tn
+// columns, tiles % mtiles counting along the rows) as four waves' float4 (i, j) of lane l at (i tn + j) 64 + l, which holds
+// rows 16 i + 4 (l / 16) .. + 3 of the tile and column 16 (wave tn + j) + l % 16.
+struct F32Partials {
+    const float* part;
+    int tm, tn, mtiles, tiles, ksplit;
+};
+// left: where every tile is split, their sums are the caller's, from *left (else it stays as it was).
 int launch_gemm_f32(const float* A, int64_t lda, const void* W, int w_type, int64_t ldw, const float* C, int64_t ldc,
-                    float* Out, int64_t ldo, int64_t M, int64_t N, int64_t K, void* ws, size_t ws_bytes, hipStream_t s);
+                    float* Out, int64_t ldo, int64_t M, int64_t N, int64_t K, void* ws, size_t ws_bytes, hipStream_t s, F32Partials* left = nullptr);
 // Decode GEMM whose masked input fl32(X + eta) is formed in-kernel from X and a
 // given mask eta (both M x K float32).
 int launch_skinny_masked(const float* X, int64_t ldx, const float* eta, int64_t ld_eta, int prec,

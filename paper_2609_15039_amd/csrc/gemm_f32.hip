@@ -427,7 +427,7 @@ size_t f32_gemm_workspace_bytes(int64_t M, int64_t N, int64_t K)
 }
 
 int launch_gemm_f32(const float* A, int64_t lda, const void* W, int w_type, int64_t ldw, const float* C, int64_t ldc,
-                    float* Out, int64_t ldo, int64_t M, int64_t N, int64_t K, void* ws, size_t ws_bytes, hipStream_t s)
+                    float* Out, int64_t ldo, int64_t M, int64_t N, int64_t K, void* ws, size_t ws_bytes, hipStream_t s, F32Partials* left)
 {
     if (M == 0 || N == 0) return SPLITEE_OK;
     const F32Plan p = plan_f32(M, N, K, ws != nullptr);
@@ -435,7 +435,8 @@ int launch_gemm_f32(const float* A, int64_t lda, const void* W, int w_type, int6
     float* part = p.ksplit > 1 ? ws_partials(ws) : nullptr;
     const dim3 grid((unsigned)(p.nfull + (int64_t)p.rem * p.ksplit));
     const dim3 g2((unsigned)(((int64_t)p.rem * p.tm * p.tn * 256 + 255) / 256));
-    const bool bf16 = w_type == SPLITEE_BF16;
+    const bool bf16 = w_type == SPLITEE_BF16, leave = left && p.ksplit > 1 && p.nfull == 0;
+    if (leave) *left = F32Partials{part, p.tm, p.tn, p.mtiles, p.rem, p.ksplit};
     if (p.tm == 8 && p.tn == 2) {
         if (bf16)
             hipLaunchKernelGGL((gemm_f32_kernel<8, 2, true, true>), grid, dim3(F_NT), 0, s, A, lda, W, ldw, C, ldc, Out, ldo, (int)M,
@@ -453,7 +454,7 @@ int launch_gemm_f32(const float* A, int64_t lda, const void* W, int w_type, int6
         else                                                                                                           \
             hipLaunchKernelGGL((gemm_f32_kernel<TM, TN, false>), grid, dim3(F_NT), 0, s, A, lda, W, ldw, C, ldc, Out,  \
                                ldo, (int)M, (int)N, (int)K, p.mtiles, p.nfull, p.ktps, p.rem, part);                   \
-        if (p.ksplit > 1)                                                                                              \
+        if (p.ksplit > 1 && !leave)                                                                                    \
             hipLaunchKernelGGL((f32_sum_kernel<TM, TN>), g2, dim3(256), 0, s, part, p.ksplit, C, ldc, Out, ldo,        \
                                (int)M, (int)N, p.mtiles, p.nfull, p.rem);                                              \
     } while (0)

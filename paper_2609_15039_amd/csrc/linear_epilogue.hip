@@ -5,6 +5,7 @@
 #include <algorithm>
 #include <cmath>
 
+#include "gemm_dev.hpp"
 #include "linear_plan.hpp"
 
 namespace {
@@ -37,6 +38,71 @@ __global__ void __launch_bounds__(256) linear_sum_kernel(LinArgs p, const float*
     float res[4];
     splitee::epi_residual(p, row, n, p.N - n, res);
     splitee::epi_finish<GATED, false>(p, z[0], z[GATED], res, row, n, p.N - n);
+}
+
+// The same from a binary32 GEMM's partial tiles (F32Partials): a wave takes 16 rows x 16 columns, a lane four rows of a
+// column, all splits of them in flight together, C, bias and the residual too, and adds in the GEMM's order.  40 x 4096 x 2560
+// with everything 17.8 us, with the sum and the epilogue in launches of their own 21.3; one row 2560 x 9728 17.2 and 20.1.
+constexpr int FP_MAX_KS = 16;
+template <bool GATED, int TN>
+__global__ void __launch_bounds__(256) f32_partials_kernel(LinArgs p, splitee_host::F32Partials f, int colblocks)
+{
+    const int lane = threadIdx.x % 64, b = blockIdx.x * 4 + threadIdx.x / 64;
+    const int rb = b / colblocks, row0 = 16 * rb + 4 * (lane / 16), col = 16 * (b % colblocks) + lane % 16;
+    if (16 * rb >= p.rows) return;
+    constexpr int H = GATED ? 2 : 1;
+    float cv[H][4], bias[H], res[4];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        bias[h] = p.bias ? p.bias[col < p.N ? h * p.N + col : 0] : 0.f;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            cv[h][r] = p.C ? p.C[row0 + r < p.rows && col < p.N ? (int64_t)(row0 + r) * p.ldc + h * p.N + col : 0] : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int64_t at = row0 + r < p.rows && col < p.N ? (int64_t)(row0 + r) * p.ldres + col : 0;
+        res[r] = !p.res ? 0.f
+                 : p.out_bf16 ? splitee::bf16_bits_to_f32(reinterpret_cast<const uint16_t*>(p.res)[at])
+                              : reinterpret_cast<const float*>(p.res)[at];
+    }
+    const int per = f.tm * TN * 64; // float4 of a wave's partial
+    const __amdgpu_buffer_rsrc_t rp = make_rsrc(f.part, (uint32_t)((int64_t)f.tiles * f.ksplit * per * 64));
+    f32x4_t v[H][FP_MAX_KS];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+        const int c = h * p.N + min(col, p.N - 1), in = c % (64 * TN);
+        const int tile = c / (64 * TN) * f.mtiles + rb / f.tm;
+        const int e = in / (16 * TN) * per + (rb % f.tm * TN + in / 16 % TN) * 64 + lane / 16 * 16 + c % 16;
+#pragma unroll
+        for (int q = 0; q < FP_MAX_KS; ++q)
+            v[h][q] = __builtin_bit_cast(f32x4_t, load16(rp, q < f.ksplit ? (uint32_t)((q * f.tiles + tile) * 4 * per + e) * 16 : OOB));
+    }
+    float z[H][4];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+#pragma unroll
+        for (int q = 1; q < FP_MAX_KS; ++q)
+            if (q < f.ksplit) v[h][0] += v[h][q];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            z[h][r] = v[h][0][r];
+            if (p.C) z[h][r] -= cv[h][r];
+            if (p.bias) z[h][r] += bias[h];
+        }
+    }
+    splitee::epi_act(z[0], p.act);
+    if (col >= p.N) return;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        if (row0 + r >= p.rows) return;
+        float h = z[0][r];
+        if (GATED) h *= z[H - 1][r];
+        if (p.res) h += res[r];
+        const int64_t at = (int64_t)(row0 + r) * p.ldy + col;
+        if (p.out_bf16) reinterpret_cast<uint16_t*>(p.Y)[at] = (uint16_t)splitee::bf16_bits_rne(h);
+        else reinterpret_cast<float*>(p.Y)[at] = h;
+    }
 }
 
 }  // namespace
@@ -136,6 +202,17 @@ int launch_sum(const LinArgs& p, const float* part, int ksplit, hipStream_t s)
     return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
 }
 
+int launch_f32_partials(const LinArgs& p, const F32Partials& f, hipStream_t s)
+{
+    const int64_t colblocks = (p.N + 15) / 16, wgs = ((int64_t)(p.rows + 15) / 16 * colblocks + 3) / 4;
+    if (!launch_fits(wgs, 256)) return SPLITEE_ERR_UNSUPPORTED;
+#define FP_RUN(GATED, TN) hipLaunchKernelGGL((f32_partials_kernel<GATED, TN>), dim3((unsigned)wgs), dim3(256), 0, s, p, f, (int)colblocks)
+    if (p.gated) { if (f.tn == 1) FP_RUN(true, 1); else FP_RUN(true, 2); }
+    else { if (f.tn == 1) FP_RUN(false, 1); else FP_RUN(false, 2); }
+#undef FP_RUN
+    return hipGetLastError() == hipSuccess ? SPLITEE_OK : SPLITEE_ERR_HIP;
+}
+
 int launch_dense_f32(const LinArgs& p, int w_type, void* ws, hipStream_t s)
 {
     if (!launch_fits(sum_workgroups(p), 256)) return SPLITEE_ERR_UNSUPPORTED;
@@ -145,11 +222,14 @@ int launch_dense_f32(const LinArgs& p, int w_type, void* ws, hipStream_t s)
         return launch_gemm_f32(A, p.lda, p.W, w_type, p.ldw, p.C, p.ldc, reinterpret_cast<float*>(p.Y), p.ldy, p.rows, p.N, p.K, ws,
                                d.gemm, s);
     float* R = reinterpret_cast<float*>(reinterpret_cast<char*>(ws) + d.gemm);
+    F32Partials left{};
     for (int h = 0; h < d.halves; ++h) {
         const char* W = reinterpret_cast<const char*>(p.W) + (int64_t)h * p.N * p.ldw * (w_type == SPLITEE_F32 ? 4 : 2);
-        const int rc = launch_gemm_f32(A, p.lda, W, w_type, p.ldw, nullptr, 0, R + h * (d.ld / 2), d.ld, p.rows, d.n, p.K, ws, d.gemm, s);
+        const int rc = launch_gemm_f32(A, p.lda, W, w_type, p.ldw, nullptr, 0, R + h * (d.ld / 2), d.ld, p.rows, d.n, p.K, ws, d.gemm, s,
+                                       d.halves == 1 ? &left : nullptr);
         if (rc != SPLITEE_OK) return rc;
     }
+    if (left.part) return launch_f32_partials(p, left, s); // (all tiles split: rows few enough)
     return launch_sum(p, R, 1, s);
 }
 

@@ -1,6 +1,6 @@
 // Binary32 products by expert with an epilogue (gfx950), W float32 or bfloat16 (widened exactly) row-major.
-// (The dense ones are the binary32 GEMM's, followed by the epilogue as a launch of its own: at 120-130 of 154
-// TFLOP/s its second pass over the product costs 4% at 1000 rows of gate/up.)
+// (The dense ones are the binary32 GEMM's, followed by the epilogue with the sum of its splits or as a launch of its own: at 120-130 of 154
+// TFLOP/s the latter's second pass over the product costs 4% at 1000 rows of gate/up.)
 //
 // Bound by the matrix cores (v_mfma_f32_16x16x4_f32, 154 TFLOP/s) for many rows an expert, by W for few.  Tiles of 16
 // or 64 rows x 64 outputs; both operands by 16-byte loads to LDS, three 32-k stages, swizzled; the four waves lie side

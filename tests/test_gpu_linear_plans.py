@@ -49,6 +49,28 @@ def test_dense(M, N, K, prec, layout):
         assert torch.equal(Y, want)
 
 
+# few tiles under a long K: every tile is split, by tiles of one to seven 16-row blocks and one or two 64-column blocks,
+# and some that are not (the first, and gated widths that are no multiple of 4)
+@pytest.mark.parametrize("w", [F32, BF16])
+@pytest.mark.parametrize("M,N,K", [(5, 40, 64), (1, 17, 1032), (2, 2052, 4096), (17, 1000, 4096), (33, 1036, 2056), (49, 2052, 4096),
+                                   (65, 2052, 4096), (97, 2052, 4096), (257, 515, 2056), (257, 2052, 4096), (300, 2052, 4096),
+                                   (300, 2600, 4096)])
+def test_dense_binary32(M, N, K, w):
+    A, W2 = ints((M, K), -8, 8, M), ints((2 * N, K), -4, 4, N).to(w)
+    for gated, out, parts in ((False, BF16, "Cbr"), (True, F32, "Cbr"), (True, BF16, "b"), (False, F32, "r")):
+        print(M, N, K, w, gated, out, parts, flush=True)
+        NW = 2 * N if gated else N
+        C = rows_of(ints((M, NW), -50, 50, 1), F32) if "C" in parts else None
+        bias = ints((NW,), -9, 9, 2) if "b" in parts else None
+        res = rows_of(ints((M, N), -99, 99, 3), out) if "r" in parts else None
+        want = R.epilogue_bits(A.double() @ W2[:NW].double().T, C, bias, "relu", gated, res, out)
+        Y = fresh(M, N, out) if res is None else res  # the residual in place
+        beside = Y._base[:, N:].clone()
+        sp.linear_epilogue(A, sp.SPLITEE_PREC_F32, W2[:NW], C=C, bias=bias, act="relu", gated=gated, residual=res, out_dtype=out, Y=Y)
+        assert torch.equal(Y, want)
+        assert torch.equal(Y._base[:, N:].view(torch.uint8), beside.view(torch.uint8))
+
+
 @pytest.mark.parametrize("layout", ["rows", "tiled"])
 @pytest.mark.parametrize("prec", ["bf16", "bf16x3"])
 @pytest.mark.parametrize("at", range(len(GROUPED)))
