@@ -209,10 +209,17 @@ class TiledWeights:
         return self.data.data_ptr()
 
 
-def _wtype(W):
+def _wtype(W, name="W"):
+    """w_type of a weight tensor; any other type would be read as one of these, and past its end."""
     if isinstance(W, TiledWeights):
+        if W.data.dtype != torch.bfloat16 and W.data.dtype.is_floating_point:  # (integers hold its bytes)
+            raise ValueError("%s: tiled weights are bfloat16, not %s" % (name, W.data.dtype))
         return SPLITEE_BF16_TILED
-    return SPLITEE_BF16 if W.dtype == torch.bfloat16 else SPLITEE_F32
+    if W.dtype == torch.bfloat16:
+        return SPLITEE_BF16
+    if W.dtype != torch.float32:
+        raise ValueError("%s: expected float32 or bfloat16, not %s" % (name, W.dtype))
+    return SPLITEE_F32
 
 
 # ------------------------------------------------------------ C entry points
@@ -561,6 +568,7 @@ def workspace(M, N, K, prec, device="cuda", gemm_only=False):
 
 def tile_weights(W):
     """W (N x K bfloat16, row-major) in the tiled order, as TiledWeights."""
+    _expect(W.dtype == torch.bfloat16, "W: expected bfloat16")
     N, K = W.shape
     data = torch.empty(splitee_tiled_weights_bytes(N, K) // 2, dtype=torch.bfloat16, device=W.device)
     splitee_tile_weights(W, W.stride(0), N, K, data)
@@ -738,9 +746,10 @@ def linear_epilogue(A, prec, W, C=None, bias=None, act="none", gated=False, resi
     NW = W.shape[0]
     _expect(len(W.shape) == 2 and W.shape[1] == K, "W: expected N x %d" % K)
     _expect(W.stride(1) == 1 or K <= 1, "W: columns are not contiguous")
-    N = _out_width(NW, gated)
-    if isinstance(W, TiledWeights):
-        _expect(not M or W.data.numel() >= _tiled_elements(NW, K), "W: fewer elements than its tiled order has")
+    N, w_type = _out_width(NW, gated), _wtype(W)
+    if w_type == SPLITEE_BF16_TILED:
+        _expect(not M or W.data.is_contiguous() and W.data.numel() * W.data.element_size() >= 2 * _tiled_elements(NW, K),
+                "W: less in one piece than its tiled order has")
     dev = _here(A, W.data if isinstance(W, TiledWeights) else W, C, bias, residual, Y)
     if bias is not None:
         _expect(tuple(bias.shape) == (NW,) and bias.dtype == torch.float32 and (NW < 2 or bias.stride(0) == 1),
@@ -757,7 +766,7 @@ def linear_epilogue(A, prec, W, C=None, bias=None, act="none", gated=False, resi
     else:
         ws, nbytes = _ptr(ws[0]), ws[1]
     _check("splitee_linear_epilogue", lib.splitee_linear_epilogue(
-        A.data_ptr(), prec, lda, W.data_ptr(), _wtype(W), W.stride(0) if NW > 1 and K else K, ctypes.byref(ep), Y.data_ptr(), ldy,
+        A.data_ptr(), prec, lda, W.data_ptr(), w_type, W.stride(0) if NW > 1 and K else K, ctypes.byref(ep), Y.data_ptr(), ldy,
         M, N, K, ws, nbytes, torch._C._cuda_getCurrentRawStream(dev)))
     return Y
 
@@ -772,15 +781,16 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
     _expect(len(W.shape) == (2 if tiled else 3) and W.shape[-1] == K, "W: expected experts x N x %d" % K)
     experts = (W.data if tiled else W).shape[0]
     NW = W.shape[-2]
-    N = _out_width(NW, gated)
+    N, w_type = _out_width(NW, gated), _wtype(W)
+    if tiled:
+        _expect(W.data.dim() == 2 and W.data.element_size() == 2 and W.data.shape[1] >= _tiled_elements(NW, K)
+                and W.data.stride(1) == 1, "W: expected experts x bfloat16 elements of tiled weights")
     dev = _here(A, W.data if tiled else W, offsets, row_index, C, bias, residual, Y)
     for name, t, n in (("offsets", offsets, experts + 1), ("row_index", row_index, None)):
         _expect(t is None or t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous() and n in (None, t.numel()),
                 "%s: expected contiguous int32%s" % (name, " of experts + 1" if n else ""))
     rows = a_rows if row_index is None else row_index.numel()
     if tiled:
-        _expect(W.data.dim() == 2 and W.data.shape[1] >= _tiled_elements(NW, K) and W.data.stride(1) == 1,
-                "W: expected experts x elements of tiled weights")
         ldw, w_stride = K, W.data.stride(0)
     else:
         _expect(W.stride(2) == 1 or K <= 1, "W: columns are not contiguous")
@@ -795,7 +805,7 @@ def grouped_linear(A, prec, W, offsets, row_index=None, C=None, bias=None, act="
         ldy = _matrix("Y", Y, (rows, N), out_dtype)
     _check("splitee_grouped_linear", load().splitee_grouped_linear(
         A.data_ptr(), prec, lda, a_rows, None if row_index is None else row_index.data_ptr(), offsets.data_ptr(), experts,
-        W.data_ptr(), _wtype(W), ldw, w_stride, ctypes.byref(ep), Y.data_ptr(), ldy, rows, N, K,
+        W.data_ptr(), w_type, ldw, w_stride, ctypes.byref(ep), Y.data_ptr(), ldy, rows, N, K,
         torch._C._cuda_getCurrentRawStream(dev)))
     return Y
 
@@ -892,6 +902,8 @@ def expert_ffn(X, logits, k, W_gate_up, W_down, mech=SPLITEE_MECH_NONE, sensitiv
     D, N = W_down.shape[-2:]
     _expect(logits.dim() == 2 and logits.shape[0] == T, "logits: expected %d tokens x experts" % T)
     _expect(tuple(W_gate_up.shape[-2:]) == (2 * N, K), "W_gate_up: expected experts x %d x %d" % (2 * N, K))
+    _wtype(W_gate_up, "W_gate_up")
+    _wtype(W_down, "W_down")
     if residual is not None:
         _matrix("residual", residual, (T, D), out_dtype)
     _here(X, logits, residual, *(W.data if isinstance(W, TiledWeights) else W for W in (W_gate_up, W_down)))
