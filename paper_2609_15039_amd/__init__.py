@@ -814,6 +814,7 @@ def tile_experts(W):
     """experts x N x K bfloat16 in the tiled order, an expert a row of the TiledWeights' data."""
     _expect(W.dim() == 3 and W.dtype == torch.bfloat16 and (W.stride(2) == 1 or W.shape[2] <= 1),
             "W: expected bfloat16 of experts x N x K, columns contiguous")
+    _here(W)
     E, N, K = W.shape
     data = torch.empty((E, splitee_tiled_weights_bytes(N, K) // 2), dtype=torch.bfloat16, device=W.device)
     for e in range(E):
