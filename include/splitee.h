@@ -320,7 +320,8 @@ int splitee_correction(float* C, int64_t ldc, const void* W, int w_type, int64_t
  * every step in binary32; C, bias and residual may each be NULL (left out).  act, of one z:
  *     NONE z;  SILU z / (1 + exp(-z));  GELU z (1 + erf(z / sqrt 2)) / 2;  RELU max(z, 0);
  *     GELU_TANH z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2
- * (a NaN stays a NaN, RELU's too; SILU and GELU of -inf are NaN, as the formulas say).
+ * (a NaN stays a NaN, RELU's too; SILU and GELU of -inf are NaN, as the formulas say).  act itself, as evaluated, is
+ * off by less than 16 2^-24 |z|, GELU by less than 13 2^-24 of its value where z >= -1.4.
  * Like the fused call's unmask, the epilogue computes on this GPU what the paper's deployment
  * leaves to the trusted side.
  */
