@@ -398,7 +398,8 @@ int splitee_grouped_linear(const void* A, int in_prec, int64_t lda, int64_t a_ro
  *               expert: it is not chosen, and its score is 0.  +inf is chosen first, in a SOFTMAX with NaN for
  *               the token's weights, as the formula says (a SIGMOID's is 1)
  *   score       SOFTMAX: exp(l - max l) / sum over the row's experts; SIGMOID: 1 / (1 + exp(-l))
- *   renorm      != 0: the chosen weights are divided by their sum (left 0 where that is 0)
+ *   renorm      != 0: the chosen weights are divided by their sum (left 0 where that is 0).  A SIGMOID's score of a
+ *               logit below -700 counts as 0; without renorm one below 2^-126 may be 0 as a weight
  *   experts     out, T x k int32: the k largest logits in falling order, equal ones by rising index;
  *               -1 where fewer than k are not masked (a padding token: all of them)
  *   weights     out, T x k float32; 0 beside -1

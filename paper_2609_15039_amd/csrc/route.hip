@@ -174,9 +174,13 @@ route_topk_kernel(const float* __restrict__ logits, int64_t ldl, int T, int E, i
             if (i >= tokens) break;
             const int64_t t = t0 + i;
             const float b = of_key(best[q]);
-            float w = mine[q] < 0 ? 0.f : score == SPLITEE_SCORE_SOFTMAX ? expf(b - m[q]) : 1.0f / (1.0f + expf(-b));
+            // of low sigmoids only the quotients matter, which exp(-m) times each has too: exp(-b) overflows from 88.7 on
+            const bool soft = score == SPLITEE_SCORE_SOFTMAX, low = !soft && renorm && m[q] < 0.f;
+            float w = soft || low ? expf(b - m[q]) : 1.0f;
+            if (!soft) w = low && b < -700.f ? 0.f : w / (1.0f + expf(low ? b : -b));
+            if (mine[q] < 0) w = 0.f;
             const float sum = renorm ? wave_sum(w) : total[q];
-            if ((renorm || score == SPLITEE_SCORE_SOFTMAX) && sum != 0.f) w = w / sum;
+            if ((renorm || soft) && sum != 0.f) w = w / sum;
             if (lane < k) {
                 experts[t * k + lane] = mine[q];
                 weights[t * k + lane] = mine[q] < 0 ? 0.f : w;
