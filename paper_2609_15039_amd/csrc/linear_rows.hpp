@@ -1,6 +1,6 @@
 // Few rows of bfloat16 products with an epilogue on the matrix cores (gfx950), dense and by expert.
 //
-// Bound by W, read once from HBM.  A workgroup owns BM rows (8, 16 or 32) and 16 TN weight rows (gated: half of
+// Bound by W, read once from HBM.  A workgroup owns BM rows (8 or 16) and 16 TN weight rows (gated: half of
 // them gate, half up rows of the same outputs); its waves split K: wave w takes the 64-k tiles w, w + NW, ..,
 // and the waves' sums meet in LDS and are added in wave order, so that the result does not depend on timing and
 // no other workgroup is waited for.  W goes straight to the registers that the MFMA reads, two K tiles ahead; the rows
@@ -34,7 +34,6 @@ __global__ void __launch_bounds__(NW * WAVE)
 lin_rows_kernel(const LinArgs p, const int ntiles)
 {
     constexpr int R = 2;                        // K tiles ahead
-    constexpr int MT = (BM + 15) / 16;          // 16-row blocks of the MFMA
     constexpr int LA = NPL * BM / 8, LW = 2 * TN; // loads per K tile
     constexpr int TO = GATED ? TN / 2 : TN, BN = 16 * TN, BNO = 16 * TO;
     // LDS of a wave's stage: planes of BM rows; 8 rows fill half of a 16-row block, whose other rows hold whatever the next
@@ -42,6 +41,7 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
     constexpr int SB = NPL * BM * 128, SBP = BM < 16 ? SB + 1024 : SB;
     constexpr int LDR = BN + 4, RB = NW * BM * LDR * 4;
     constexpr int NT = NW * WAVE;
+    static_assert(BM == 8 || BM == 16, "one 16-row block of the MFMA");
     static_assert(!GATED || TN % 2 == 0, "gate and up blocks in pairs");
     static_assert((R - 1) * (LA + LW) < 64, "loads in flight exceed the wait counter");
     const int tid = threadIdx.x, lane = tid % WAVE;
@@ -109,31 +109,25 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
 #pragma unroll
     for (int u = 0; u < R; ++u) issue(u, u);
 
-    f32x4_t acc[2][MT][TN];
+    f32x4_t acc[2][TN];
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) acc[s][i][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < TN; ++j) acc[s][j] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     auto consume = [&](int u) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            uint4 a[NPL][MT];
+            uint4 a[NPL];
+#pragma unroll
+            for (int pl = 0; pl < NPL; ++pl) {
+                const int row = pl * BM + fr;
+                a[pl] = *reinterpret_cast<const uint4*>(st[u] + wave * SBP + row * 128 + (((4 * s + fq) ^ ((row >> 1) & 7)) << 4));
+            }
 #pragma unroll
             for (int pl = 0; pl < NPL; ++pl)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const int row = pl * BM + 16 * i + fr;
-                    a[pl][i] = *reinterpret_cast<const uint4*>(st[u] + wave * SBP + row * 128 + (((4 * s + fq) ^ ((row >> 1) & 7)) << 4));
-                }
-#pragma unroll
-            for (int pl = 0; pl < NPL; ++pl)
-#pragma unroll
-                for (int i = 0; i < MT; ++i)
-#pragma unroll
-                    for (int j = 0; j < TN; ++j)
-                        acc[s][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a[pl][i]), as_bf16x8(wr[u][s][j]), acc[s][i][j], 0, 0, 0);
+                for (int j = 0; j < TN; ++j)
+                    acc[s][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(as_bf16x8(a[pl]), as_bf16x8(wr[u][s][j]), acc[s][j], 0, 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -156,14 +150,12 @@ lin_rows_kernel(const LinArgs p, const int ntiles)
     float* const red = reinterpret_cast<float*>(RB <= NW * SBP ? st[0] : lr_stage<2, RB <= NW * SBP ? 16 : RB>());
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
+    for (int j = 0; j < TN; ++j) {
+        const f32x4_t v = acc[0][j] + acc[1][j];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-            const f32x4_t v = acc[0][i][j] + acc[1][i][j];
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (16 * i + 4 * fq + r < BM) red[(wave * BM + 16 * i + 4 * fq + r) * LDR + 16 * j + fr] = v[r];
-        }
+        for (int r = 0; r < 4; ++r)
+            if (4 * fq + r < BM) red[(wave * BM + 4 * fq + r) * LDR + 16 * j + fr] = v[r];
+    }
     __syncthreads();
     const int rows = min(BM, g.end - m0);
     for (int f = tid; f < rows * BNO; f += NT) {
