@@ -186,10 +186,16 @@ int f32_run(const LinArgs& p, bool bf16, hipStream_t s)
 
 namespace splitee_host {
 
-// 16-row tiles up to 24 rows an expert on average, else 64-row tiles.
+// 16-row tiles up to 48 rows an expert on average (float32 W, whose every row tile costs twice the loads: 32), else 64-row
+// tiles, which read W once for four times the rows but are fewer and, gated, leave a CU's LDS room for one workgroup.  Both sides, us,
+// 16- and 64-row tiles, 2048 x 768, gated and not:
+//   bfloat16 W, 32 experts  24 rows 84 182, 58 80;  48 rows 150 184, 82 81;  64 rows 170 269, 109 134
+//               64 experts  24 rows 172 301, 86 148;  48 rows 252 363, 148 158;  8 of 4096 x 2560, 64 rows 371 352, 156 154
+//   float32 W, 32 experts   24 rows 149 190, 71 87;  32 rows 153 190, 84 88;  36 rows 208 191, 127 88;  48 rows 218 191, 134 89
+//               64 experts  32 rows 318 372, 162 164;  40 rows 380 373, 210 166
 int launch_grouped_f32(const splitee::LinArgs& p, bool w_bf16, hipStream_t s)
 {
-    const bool few = (int64_t)p.rows <= 24 * (int64_t)p.experts;
+    const bool few = (int64_t)p.rows <= (w_bf16 ? 48 : 32) * (int64_t)p.experts;
     if (p.gated) return few ? f32_run<1, true>(p, w_bf16, s) : f32_run<4, true>(p, w_bf16, s);
     return few ? f32_run<1, false>(p, w_bf16, s) : f32_run<4, false>(p, w_bf16, s);
 }
