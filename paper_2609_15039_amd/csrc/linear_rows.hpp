@@ -8,8 +8,8 @@
 // wave: no barrier in the loop.  Two K tiles ahead: three and four were slower (one token of 2 x 9728 x 2560 17.6, 21.8 and
 // 23.7 us, W then partly in caches), and so were 32-row tiles (32 rows in three planes 34 us, twice 16 rows 33).
 //
-// One token of 2 x 9728 x 2560, three planes, gated, with its correction: 19.8 us (5.0 TB/s of W); one token of 2560 x 9728
-// 12.5; 64 rows of 64 experts, 2 x 768 x 2048, bfloat16: 46 us (about 5.4 TB/s of the experts that have rows).
+// One token of 2 x 9728 x 2560, three planes, gated, with its correction: 19.8 us (5.0 TB/s of W), 21.5 where none of W is in
+// a cache; one token of 2560 x 9728 12.5; 64 rows of 64 experts, 2 x 768 x 2048, bfloat16: 46 us (about 5.4 TB/s of the experts that have rows).
 #pragma once
 #include "linear_tile.hpp"
 

@@ -9,8 +9,9 @@
 // What bounds it: the operand tiles that every CU takes from its L2 (64 KB for 256 x 256 x 64: about 1.05 us without
 // the MFMAs), which take the MFMAs' time (1.05 us at the 1.6 PFLOP/s that the matrix cores sustain on such data, 1.3 with
 // their LDS reads and barriers) to 1.5; and a tile's beginning and end, 4 and 5 us, when nothing is multiplied.  4096 x 2560
-// x 9728 with bias and GELU 191 us (1.07 PFLOP/s, the MFMAs busy half of the cycles, CUs 87%); 1000 x 2560 x 2 x 9728 in three planes,
-// gated, 277 us (1.08, busy 60%); 48000 rows of 64 experts x 2048 x 2 x 768 335 us (0.90, 49%).
+// x 9728 with bias and GELU 188 us (1.09 PFLOP/s, the MFMAs busy 49% of the cycles, CUs 87%; 223 with operands from HBM, not the
+// Infinity Cache); 1000 x 2560 x 2 x 9728 in three planes, gated, 272 us (1.10, busy 50%); 48000 rows of 64 experts x 2048 x 2 x 768
+// 332 us (0.91, 45%).
 // Built and measured against it, not kept: a ring of five operand slots instead of two stages (84 us against 80 for 4096 x
 // 4096 x 2560), four waves of 128 x 128 (their accumulators do not stay in registers), wave priority around the MFMAs (within 1%),
 // C's lines touched when a tile begins (277 against 273), 128 x 128 tiles, two workgroups a CU (383 against 340 for the experts).
